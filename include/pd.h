@@ -410,6 +410,95 @@ PD_API pd_status pd_cross_attention_static(int32_t dtype, int32_t batch, int32_t
 PD_API pd_status pd_cross_attention_static_status(void *cuda_stream, int32_t *status_out);
 PD_API const char *pd_static_last_error(void);
 
+/* Rotary positions alone, on caller-supplied heads and without a handle (the decoder's own path rotates whole heads with
+ * neighbouring dims paired, unscaled, inside its projection kernels).  Of every head the first rot_dim dims are rotated
+ * in pairs (a, b) - (2 i, 2 i + 1) if interleaved, else (i, i + rot_dim / 2) - and the others copied:
+ *   t = 2 pi positions[token] turns[i],  y_a = amplitude (x_a cos t - x_b sin t),  y_b = amplitude (x_a sin t + x_b cos t)
+ * with t -> -t if inverse (the map's transpose: the gradient of x from that of y).  Angles are reduced in 64 bits: far positions
+ * are as exact as near ones.
+ *   dtype       PD_DTYPE_FP32 or PD_DTYPE_BF16: element type of x and out; the arithmetic is fp32, rounded once
+ *   sizes       tokens >= 0; d_head 2..256; rot_dim even, 2..d_head
+ *   x, out      device; element (token, head, dim) at token * token_stride + head * head_stride + dim (strides in elements, not
+ *               negative; x may repeat, heads of out must not overlap).  Slices of a fused projection's rows will do.  out may be x
+ *               with the same strides, else they must not overlap.  Addresses and strides that are multiples of 16 bytes,
+ *               with rot_dim / 2 (interleaved: rot_dim) and d_head multiples of 16 bytes too, take the fast path
+ *   positions   device int32 [tokens], any sign;  turns  device double [rot_dim / 2]: turns per position of every pair
+ * pd_rotary_turns fills turns (host [rot_dim / 2]) and *amplitude (host or NULL): theta^(-2 i / rot_dim) / 2 pi,
+ *   PD_ROTARY_PLAIN     as it is
+ *   PD_ROTARY_LINEAR    divided by factor >= 1 (positions squeezed)
+ *   PD_ROTARY_BY_PARTS  divided by factor for pairs that make at most slow_turns turns over original_len positions, as it is for those that
+ *                       make at least fast_turns, a ramp over the pair index between; amplitude 0.1 ln(factor) + 1
+ *                       (the scaling of arXiv 2309.00071; 32 and 1 turns there)
+ * pd_rotary enqueues on cuda_stream and returns; allocates nothing on the device.  PD_ERR_ARG for null pointers, misaligned
+ * buffers, overlapping output heads or sizes out of range, PD_ERR_CUDA if a launch fails.  pd_rotary_turns is a pure function. */
+enum { PD_ROTARY_PLAIN = 0, PD_ROTARY_LINEAR = 1, PD_ROTARY_BY_PARTS = 2 };
+PD_API pd_status pd_rotary_turns(int32_t rot_dim, double theta, int32_t scaling, double factor, int32_t original_len, double fast_turns,
+                                 double slow_turns, double *turns, float *amplitude);
+PD_API pd_status pd_rotary(int32_t dtype, int32_t tokens, int32_t n_heads, int32_t d_head, int32_t rot_dim, int32_t interleaved,
+                           int32_t inverse, const void *x, int64_t x_token_stride, int64_t x_head_stride, const int32_t *positions,
+                           const double *turns, float amplitude, void *out, int64_t out_token_stride, int64_t out_head_stride,
+                           void *cuda_stream);
+
+/* A paged cache of keys and values in 8 bits, without a handle: blocks of PD_CACHE_BLOCK tokens, E4M3 codes, one scale for each
+ * (block, head, keys | values).  kv_c_dtype = PD_KV_E4M3 has one scale for a sequence's whole context, which must be
+ * there before the first code is written; here tokens can follow one by one, and a block of large values spoils no other.
+ *   codes   device uint8 [n_blocks, n_kv_heads, 2, 4096], 16-byte aligned: a block's keys as [token][64], then its values as [64][token]
+ *   scales  device fp32 [n_blocks, n_kv_heads, 2], powers of two: value = code * scale
+ *   table   device int32 [batch, max_blocks]: position p of sequence b is token p % PD_CACHE_BLOCK of block table[b][p / PD_CACHE_BLOCK]
+ *
+ * pd_cache_append writes positions pos_start[b] .. pos_start[b] + n_new[b] - 1 of every sequence from rows row_start[b] .. of k and v:
+ *   scale = the least 2^e, e >= -126, with max |new value of the block| <= 448 * 2^e; where the block holds older tokens
+ *           of the sequence, not less than its scale so far, and their codes are rounded to the new one
+ *   code  = the nearest E4M3 value to value / scale, ties to even (NaN stays NaN; infinities set no scale and become 448)
+ * Tokens of the block behind the new ones, other blocks and their scales stay as they were.  Both scales and codes are exact: they depend
+ * on the values and on how the tokens were split over calls (through the older codes), on nothing else.
+ *   dtype      PD_DTYPE_FP32 or PD_DTYPE_BF16: element type of k and v
+ *   k, v       device [rows, n_kv_heads, 64], 16-byte aligned; k_stride, v_stride elements from row to row (at least
+ *              n_kv_heads * 64, multiples of 16 bytes): slices of a fused projection will do
+ *   row_start, n_new, pos_start   device int32 [batch]; n_new <= max_new (host), which sizes the launch; n_new = 0: nothing
+ *   status     device int32 or NULL: set to PD_ERR_ARG, and otherwise left alone, when a sequence's rows are not within 0 .. rows,
+ *              n_new is above max_new or pos_start negative (the sequence is skipped), or a block lies behind the table or
+ *              outside 0 .. n_blocks (its tokens are dropped).  Nothing outside the tensors is touched
+ * A block belongs to one sequence of a call, and calls that write one block are ordered by the caller.
+ * Enqueues on cuda_stream and returns; allocates nothing on the device.  PD_ERR_ARG for null pointers, misaligned
+ * buffers or sizes out of range, PD_ERR_CUDA if a launch fails. */
+enum { PD_CACHE_BLOCK = 64 };
+PD_API pd_status pd_cache_append(int32_t dtype, int32_t batch, int32_t n_kv_heads, int32_t n_blocks, int32_t max_blocks, int32_t rows,
+                                 int32_t max_new, const void *k, int64_t k_stride, const void *v, int64_t v_stride,
+                                 const int32_t *row_start, const int32_t *n_new, const int32_t *pos_start, const int32_t *table,
+                                 void *codes, float *scales, int32_t *status, void *cuda_stream);
+
+/* Attention of a step's rows over that cache: pd_cross_attention's counterpart.  Row (b, r), r < n_rows[b], sees the positions
+ * begin <= p < end of sequence b that hold tokens (p < lens[b]):
+ *   score = attn_scale * q . k_p;  softcap > 0: softcap * tanh(score / softcap);  bias: + bias[head][min(end - 1 - p, n_bias - 1)]
+ *   out   = softmax over those p of score . v
+ * and is zero where it sees nothing; rows at or beyond n_rows[b] are not read and come back as zeros.  Query head h reads
+ * key head h / (n_heads / n_kv_heads).
+ *   dtype      PD_DTYPE_FP32 or PD_DTYPE_BF16: element type of q and out.  bf16: scores and sums in fp32, weights rounded to f16 (11 bits);
+ *              fp32: queries and weights in two f16 parts (22 bits)
+ *   sizes      rows_per_seq 1..64; n_heads a multiple of n_kv_heads, at most 1024; max_len >= 0: host bound on lens, sizes the launch
+ *   q          device, row (b, r) at (b * rows_per_seq + r) * q_stride (at least n_heads * 64, a multiple of 16 bytes), 16-byte aligned
+ *   out        device [batch * rows_per_seq, n_heads * 64], 16-byte aligned
+ *   n_rows, lens   device int32 [batch]; clamped to 0..rows_per_seq and to 0..min(max_len, max_blocks * PD_CACHE_BLOCK)
+ *   spans      device int32 [batch, rows_per_seq, 2] = (begin, end) of every row, 8-byte aligned, clamped to 0..lens[b]; NULL = (0, lens[b]).
+ *              A causal step: end = the row's own position + 1; windows, documents and prefixes likewise
+ *   bias       device fp32 [n_heads, n_bias] or NULL: added by the distance from the end of the row's (clamped) span
+ *   scratch    device, 16-byte aligned, at least pd_cache_attention_scratch_bytes(...): partial results where a sequence is split;
+ *              needs no clearing, holds nothing between calls; calls that may overlap on the GPU need one each
+ *   status     device int32 or NULL: set to PD_ERR_ARG for a block outside 0 .. n_blocks among those that are read (its positions
+ *              count as not there), to PD_ERR_TIMEOUT if a bounded wait inside the kernel expired; otherwise left alone
+ * Codes behind a sequence's last token, and those that a row does not see, never matter, numbers or not.  Results do not depend on the other
+ * sequences of the batch, and repeat bit for bit.  Enqueues on cuda_stream and returns; allocates nothing on the device.
+ * PD_ERR_ARG for null pointers, misaligned buffers or sizes out of range, PD_ERR_WORKSPACE for a scratch that is
+ * too small, PD_ERR_CUDA if a launch fails. */
+PD_API size_t pd_cache_attention_scratch_bytes(int32_t dtype, int32_t batch, int32_t rows_per_seq, int32_t n_heads, int32_t n_kv_heads,
+                                               int32_t max_len);
+PD_API pd_status pd_cache_attention(int32_t dtype, int32_t batch, int32_t rows_per_seq, int32_t n_heads, int32_t n_kv_heads,
+                                    int32_t n_blocks, int32_t max_blocks, int32_t max_len, float attn_scale, float softcap,
+                                    const void *q, int64_t q_stride, const void *codes, const float *scales, const int32_t *table,
+                                    const int32_t *n_rows, const int32_t *lens, const int32_t *spans, const float *bias,
+                                    int32_t n_bias, void *out, void *scratch, size_t scratch_bytes, int32_t *status, void *cuda_stream);
+
 PD_API const char *pd_last_error(const pd_handle *h);
 PD_API const char *pd_version(void);
 

@@ -27,6 +27,8 @@ PD_BUF_X, PD_BUF_QKV, PD_BUF_SELF_OUT, PD_BUF_CROSS_Q, PD_BUF_CROSS_OUT, PD_BUF_
 PD_PROF_NAMES = ["append", "self_attn", "cross_attn", "argmax_sched", "gemm", "other", "vocab"]
 PD_STAT_TOKENS, PD_STAT_STEPS, PD_STAT_SELF_ENTRIES, PD_STAT_CROSS_KEYS, PD_STAT_PAGES = range(5)
 PD_STAT_COUNT = 8
+PD_CACHE_BLOCK = 64
+PD_ROTARY_PLAIN, PD_ROTARY_LINEAR, PD_ROTARY_BY_PARTS = 0, 1, 2
 LAYER_TENSORS = ["norm1", "wqkv", "wo", "norm2", "wq_c", "wkv_c", "wo_c", "norm3", "w1", "w2"]
 
 
@@ -87,6 +89,14 @@ _SIGS = {
     "pd_cross_attention_static": (C.c_int, [C.c_int32] * 5 + [C.c_float, C.c_int32] + [C.c_void_p] * 5 + [C.c_void_p]),
     "pd_cross_attention_static_status": (C.c_int, [C.c_void_p, _i32p]),
     "pd_static_last_error": (C.c_char_p, []),
+    "pd_rotary_turns": (C.c_int, [C.c_int32, C.c_double, C.c_int32, C.c_double, C.c_int32, C.c_double, C.c_double, C.POINTER(C.c_double),
+                                  C.POINTER(C.c_float)]),
+    "pd_rotary": (C.c_int, [C.c_int32] * 7 + [C.c_void_p, C.c_int64, C.c_int64, C.c_void_p, C.c_void_p, C.c_float, C.c_void_p, C.c_int64, C.c_int64,
+                                              C.c_void_p]),
+    "pd_cache_append": (C.c_int, [C.c_int32] * 7 + [C.c_void_p, C.c_int64] * 2 + [C.c_void_p] * 8),
+    "pd_cache_attention_scratch_bytes": (C.c_size_t, [C.c_int32] * 6),
+    "pd_cache_attention": (C.c_int, [C.c_int32] * 8 + [C.c_float] * 2 + [C.c_void_p, C.c_int64] + [C.c_void_p] * 7 + [C.c_int32, C.c_void_p, C.c_void_p, C.c_size_t,
+                                                                                                                   C.c_void_p, C.c_void_p]),
     "pd_last_error": (C.c_char_p, [_H]),
     "pd_version": (C.c_char_p, []),
     "pd_destroy": (None, [_H]),
@@ -506,6 +516,145 @@ def linear(a, w, mode: int = 0, row_sumsq=None, eps: float = 1e-6, x=None, gain_
         raise PdError(status, "pd_linear (device status)")
     if mode == 2:
         return xg, ssq[: parts.value]
+    return out
+
+
+def _stream_of(t) -> int:
+    """The current stream of a tensor's device, which becomes the current device of this thread's call."""
+    import torch
+    if not t.is_cuda:
+        raise ValueError("tensors must be CUDA tensors")
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError(f"tensors are on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
+    return torch.cuda.current_stream(t.device).cuda_stream
+
+
+def _dtype_of(t) -> int:
+    import torch
+    if t.dtype == torch.bfloat16:
+        return PD_DTYPE_BF16
+    if t.dtype == torch.float32:
+        return PD_DTYPE_FP32
+    raise ValueError(f"expected float32 or bfloat16, got {t.dtype}")
+
+
+def _plain(what: str, t, like, dtype, shape):
+    """A contiguous tensor of this type and shape on the device of `like`, or ValueError."""
+    if t.dtype != dtype or t.shape != shape or t.device != like.device or not t.is_contiguous():
+        raise ValueError(f"{what} must be a contiguous {dtype} tensor of shape {tuple(shape)} on {like.device}")
+    return t.data_ptr()
+
+
+def rotary_turns(rot_dim: int, theta: float = 10000.0, scaling: int = PD_ROTARY_PLAIN, factor: float = 1.0, original_len: int = 0,
+                 fast_turns: float = 32.0, slow_turns: float = 1.0):
+    """pd_rotary_turns: (turns per position of every pair, float64 numpy [rot_dim / 2]; amplitude)."""
+    turns = np.empty((max(int(rot_dim), 0) // 2,), np.float64)
+    amp = C.c_float(0)
+    st = _lib.pd_rotary_turns(rot_dim, theta, scaling, factor, original_len, fast_turns, slow_turns,
+                              turns.ctypes.data_as(C.POINTER(C.c_double)), C.byref(amp))
+    if st != PD_OK:
+        raise PdError(st, "pd_rotary_turns")
+    return turns, float(amp.value)
+
+
+def rotary(x, positions, turns, amplitude: float = 1.0, interleaved: bool = False, inverse: bool = False, out=None):
+    """pd_rotary on torch CUDA tensors: x [tokens, heads, d_head] bfloat16 or float32 (any token and head stride), positions int32
+    [tokens], turns float64 [rot_dim / 2].  Returns `out` (allocated here when not given; x itself rotates in place).  Runs on
+    torch's current stream."""
+    import torch
+    dt = _dtype_of(x)
+    if x.dim() != 3 or x.stride(2) != 1 and x.shape[2] > 1:
+        raise ValueError("x must be [tokens, heads, d_head] with neighbouring dims")
+    n, heads, dh = x.shape
+    if out is None:
+        out = torch.empty((n, heads, dh), dtype=x.dtype, device=x.device)
+    elif out.shape != x.shape or out.dtype != x.dtype or out.device != x.device or out.stride(2) != 1:
+        raise ValueError("out must have x's shape, type and device, with neighbouring dims")
+    if turns.dim() != 1:
+        raise ValueError("turns must be [rot_dim / 2]")
+    pos = _plain("positions", positions, x, torch.int32, (n,))
+    tr = _plain("turns", turns, x, torch.float64, turns.shape)
+    st = _lib.pd_rotary(dt, n, heads, dh, 2 * turns.shape[0], interleaved, inverse, x.data_ptr(), x.stride(0), x.stride(1), pos, tr, amplitude,
+                        out.data_ptr(), out.stride(0), out.stride(1), _stream_of(x))
+    if st != PD_OK:
+        raise PdError(st, "pd_rotary")
+    return out
+
+
+def _cache_args(codes, scales, table, like):
+    """(n_blocks, kv heads, max_blocks, pointers) of an 8-bit paged cache."""
+    import torch
+    if codes.dim() != 4 or table.dim() != 2:
+        raise ValueError("codes must be [blocks, kv heads, 2, 4096], table [batch, blocks of a sequence]")
+    n_blocks, heads = codes.shape[:2]
+    return (n_blocks, heads, table.shape[1], _plain("codes", codes, like, torch.uint8, (n_blocks, heads, 2, PD_CACHE_BLOCK * 64)),
+            _plain("scales", scales, like, torch.float32, (n_blocks, heads, 2)), _plain("table", table, like, torch.int32, table.shape))
+
+
+def cache_append(k, v, row_start, n_new, pos_start, table, codes, scales, max_new: int, status=None):
+    """pd_cache_append on torch CUDA tensors: k, v [rows, kv heads, 64] bfloat16 or float32 (any row stride), row_start, n_new, pos_start
+    int32 [batch], table int32 [batch, blocks], codes uint8 [blocks, kv heads, 2, 4096] and scales float32 [blocks, kv heads, 2],
+    both written in place; max_new: host bound on n_new; status: int32 [1] or None.  Runs on torch's current stream."""
+    import torch
+    dt = _dtype_of(k)
+    n_blocks, heads, max_blocks, cp, sp, tp = _cache_args(codes, scales, table, k)
+    rows, batch = k.shape[0], table.shape[0]
+    for t in (k, v):
+        if t.shape != (rows, heads, 64) or t.dtype != k.dtype or t.device != k.device or t.stride(2) != 1 or (heads > 1 and t.stride(1) != 64):
+            raise ValueError("k and v must be [rows, kv heads, 64] of one type, with neighbouring heads and dims")
+    i32 = torch.int32
+    one = heads * 64
+    st = _lib.pd_cache_append(dt, batch, heads, n_blocks, max_blocks, rows, max_new, k.data_ptr(), k.stride(0) if rows > 1 else one, v.data_ptr(),
+                              v.stride(0) if rows > 1 else one,
+                              _plain("row_start", row_start, k, i32, (batch,)), _plain("n_new", n_new, k, i32, (batch,)),
+                              _plain("pos_start", pos_start, k, i32, (batch,)), tp, cp, sp,
+                              None if status is None else _plain("status", status, k, i32, (1,)), _stream_of(k))
+    if st != PD_OK:
+        raise PdError(st, "pd_cache_append")
+
+
+def cache_attention_scratch_bytes(dtype: int, batch: int, rows_per_seq: int, n_heads: int, n_kv_heads: int, max_len: int) -> int:
+    return int(_lib.pd_cache_attention_scratch_bytes(dtype, batch, rows_per_seq, n_heads, n_kv_heads, max_len))
+
+
+def cache_attention(q, codes, scales, table, n_rows, lens, attn_scale: float, max_len: Optional[int] = None, spans=None, bias=None,
+                    softcap: float = 0.0, out=None, scratch=None, status=None):
+    """pd_cache_attention on torch CUDA tensors: q [batch, rows, heads * 64] bfloat16 or float32 (any row stride, batches rows apart),
+    the cache as in cache_append, n_rows and lens int32 [batch], spans int32 [batch, rows, 2] or None, bias float32 [heads, n] or
+    None; max_len: host bound on lens (the table's extent when not given).  `out` [batch, rows, heads * 64] and `scratch`
+    (uint8, 16-byte aligned) are allocated here when not given.  Runs on torch's current stream; returns out."""
+    import torch
+    dt = _dtype_of(q)
+    n_blocks, kv_heads, max_blocks, cp, sp, tp = _cache_args(codes, scales, table, q)
+    if q.dim() != 3 or q.shape[2] % 64 or q.stride(2) != 1 or table.shape[0] != q.shape[0]:
+        raise ValueError("q must be [batch, rows, heads * 64] with neighbouring dims, for the table's batch")
+    batch, rows, width = q.shape
+    stride = q.stride(1) if rows > 1 else q.stride(0) if batch > 1 else width       # a dimension of one has any stride
+    if batch > 1 and q.stride(0) != rows * stride:
+        raise ValueError("q's batches must lie rows apart")
+    heads = width // 64
+    if max_len is None:
+        max_len = min(max_blocks * PD_CACHE_BLOCK, (1 << 31) - 1 - PD_CACHE_BLOCK)
+    i32 = torch.int32
+    if out is None:
+        out = torch.empty((batch, rows, width), dtype=q.dtype, device=q.device)
+        op = out.data_ptr()
+    else:
+        op = _plain("out", out, q, q.dtype, (batch, rows, width))
+    if scratch is None:
+        scratch = torch.empty(_lib.pd_cache_attention_scratch_bytes(dt, batch, rows, heads, kv_heads, max_len), dtype=torch.uint8, device=q.device)
+    elif scratch.device != q.device or not scratch.is_contiguous():
+        raise ValueError("scratch must be contiguous, on q's device")
+    if bias is not None and bias.dim() != 2:
+        raise ValueError("bias must be [heads, distances]")
+    st = _lib.pd_cache_attention(dt, batch, rows, heads, kv_heads, n_blocks, max_blocks, max_len, attn_scale, softcap, q.data_ptr(), stride, cp, sp, tp,
+                                 _plain("n_rows", n_rows, q, i32, (batch,)), _plain("lens", lens, q, i32, (batch,)),
+                                 None if spans is None else _plain("spans", spans, q, i32, (batch, rows, 2)),
+                                 None if bias is None else _plain("bias", bias, q, torch.float32, (heads, bias.shape[1])),
+                                 0 if bias is None else bias.shape[1], op, scratch.data_ptr(), scratch.numel() * scratch.element_size(),
+                                 None if status is None else _plain("status", status, q, i32, (1,)), _stream_of(q))
+    if st != PD_OK:
+        raise PdError(st, "pd_cache_attention")
     return out
 
 

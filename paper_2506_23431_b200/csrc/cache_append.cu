@@ -1,0 +1,189 @@
+// Append of keys and values to a paged cache of E4M3 codes: blocks of 64 tokens, a power-of-two scale for each (block, head,
+// keys | values).  The layout is the one cache_attn.cu reads: codes [block][head][2][4096], keys as [token][dim], values as
+// [dim][token]; scales [block][head][2].
+//
+//   fresh = least 2^e, e >= -126, with max |finite new value of the block| <= 448 * 2^e
+//   scale = fresh where the call begins the block, else max(scale held, fresh)
+//   code  = RN_e4m3(x / scale), saturating;  older codes of the block: RN_e4m3(code * scale held / scale)
+//
+// A scale that is a power of two costs a format with an exponent of its own nothing but part of its subnormal range, and makes every division
+// exact: the codes do not depend on the precision they are computed in, and a block whose scale grows keeps its older
+// codes bit for bit, but for those that leave the normal range.
+//
+// One CTA per (block, head): 128 threads take the keys, 128 the values.  A thread holds four tokens of eight dims, so that it
+// writes keys as 8 bytes per token and values, whose layout is turned, as whole words of four tokens, with no pass through shared memory.
+#include <cuda_fp16.h>
+
+#include "pd_internal.h"
+
+using namespace pd;
+
+namespace {
+
+constexpr int kBlk = PD_CACHE_BLOCK;
+constexpr int kPart = kBlk * kDh;                 // codes of a block's keys (values) of one head
+
+struct AppendArgs {
+  int heads, n_blocks, max_blocks, rows, max_new;
+  const void *k, *v;
+  long long k_stride, v_stride;
+  const int32_t *row_start, *n_new, *pos_start, *table;
+  uint8_t *codes; float *scales; int32_t *status;
+};
+
+__device__ __forceinline__ uint32_t e4m3x2(float lo, float hi) {        // round to nearest even, saturating; NaN stays NaN
+  unsigned short r;
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+__device__ __forceinline__ uint32_t e4m3x4(float a, float b, float c, float d) { return e4m3x2(a, b) | e4m3x2(c, d) << 16; }
+
+// The codes of four tokens (or dims) at another scale: times f, rounded again.
+__device__ __forceinline__ uint32_t rescale4(uint32_t w, float f) {
+  uint32_t lo, hi;
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(lo) : "h"((unsigned short)w));
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(hi) : "h"((unsigned short)(w >> 16)));
+  const float2 a = __half22float2(*reinterpret_cast<__half2 *>(&lo)), b = __half22float2(*reinterpret_cast<__half2 *>(&hi));
+  return e4m3x4(a.x * f, a.y * f, b.x * f, b.y * f);
+}
+
+// Least e >= -126 with amax <= 448 * 2^e, 448 = 1.75 * 2^8; amax given by its bits.
+__device__ __forceinline__ int scale_exponent(uint32_t amax_bits) {
+  const int k = (int)(amax_bits >> 23) - 127;
+  return max(k - 8 + ((amax_bits & 0x7fffffu) > 0x600000u ? 1 : 0), -126);
+}
+__device__ __forceinline__ float pow2(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }      // -126 <= e <= 127
+
+__device__ __forceinline__ void load8(const float *p, float (&f)[8]) {
+  const float4 a = *reinterpret_cast<const float4 *>(p), b = *reinterpret_cast<const float4 *>(p + 4);
+  f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
+}
+__device__ __forceinline__ void load8(const __nv_bfloat16 *p, float (&f)[8]) {
+  const uint4 w = *reinterpret_cast<const uint4 *>(p);
+  const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    f[2 * i] = __uint_as_float(u[i] << 16);
+    f[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
+  }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(256) cache_append_kernel(AppendArgs a) {
+  const int b = blockIdx.z, h = blockIdx.y, is_v = threadIdx.x >> 7, t = threadIdx.x & 127;
+  const long long n = a.n_new[b], p0 = a.pos_start[b], row0 = a.row_start[b];
+  if (n <= 0) return;
+  const long long j = p0 / kBlk + blockIdx.x;                                     // block of the sequence
+  const int lo = (int)max(p0 - j * kBlk, 0ll), hi = (int)min(p0 + n - j * kBlk, (long long)kBlk);
+  if (p0 >= 0 && hi <= 0) return;                                                 // the sequence's tokens end before this block
+  const bool fits = n <= a.max_new && p0 >= 0 && row0 >= 0 && row0 + n <= a.rows && j < a.max_blocks;
+  const int id = fits ? a.table[(size_t)b * a.max_blocks + j] : -1;
+  if (id < 0 || id >= a.n_blocks) {
+    if (threadIdx.x == 0 && h == 0 && a.status) *a.status = PD_ERR_ARG;
+    return;
+  }
+  const size_t part = ((size_t)id * a.heads + h) * 2 + is_v;
+  // four tokens of eight dims; keys: neighbouring lanes share a token, values: they share dims
+  const int dg = is_v ? t >> 4 : t & 7, tg = is_v ? t & 15 : t >> 3;
+  const T *src = static_cast<const T *>(is_v ? a.v : a.k) + h * kDh + dg * 8;
+  const long long stride = is_v ? a.v_stride : a.k_stride, first = row0 + j * kBlk - p0 + tg * 4;
+  const float had = lo > 0 ? a.scales[part] : 0.f;
+  float f[4][8];
+  uint32_t amax = 0;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const int tok = tg * 4 + k;
+    if (tok >= lo && tok < hi) load8(src + (first + k) * stride, f[k]);
+    else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) f[k][i] = 0.f;
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const uint32_t m = __float_as_uint(f[k][i]) & 0x7fffffffu;
+      amax = max(amax, m < 0x7f800000u ? m : 0u);                                 // infinities and NaN set no scale
+    }
+  __shared__ uint32_t warp_max[8];
+  amax = __reduce_max_sync(0xffffffffu, amax);
+  if ((threadIdx.x & 31) == 0) warp_max[threadIdx.x >> 5] = amax;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < 4; ++w) amax = max(amax, warp_max[is_v * 4 + w]);
+  const float fresh = pow2(scale_exponent(amax)), scale = fmaxf(fresh, had);
+  const float inv = 1.f / scale;                                                  // exact: a power of two
+  uint8_t *dst = a.codes + part * kPart;
+  if (lo > 0 && scale > had) {                                                    // older tokens of the block move to the new scale
+    const float g = had * inv;
+    if (!is_v) {
+      for (int w = t; w < lo * (kDh / 4); w += 128) {
+        uint32_t *p = reinterpret_cast<uint32_t *>(dst) + w;
+        *p = rescale4(*p, g);
+      }
+    } else {
+      for (int w = t; w < kDh * kBlk / 4; w += 128) {
+        const int tok = (w & 15) * 4;
+        if (tok >= lo) continue;
+        uint32_t *p = reinterpret_cast<uint32_t *>(dst) + w;
+        const uint32_t r = rescale4(*p, g);
+        if (tok + 4 <= lo) *p = r;
+        else                                                                      // the word's other bytes are new tokens'
+          for (int k = 0; k < lo - tok; ++k) reinterpret_cast<uint8_t *>(p)[k] = (uint8_t)(r >> (8 * k));
+      }
+    }
+  }
+  if (tg * 4 + 4 > lo && tg * 4 < hi) {
+    if (!is_v) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int tok = tg * 4 + k;
+        if (tok >= lo && tok < hi)
+          *reinterpret_cast<uint2 *>(dst + tok * kDh + dg * 8) =
+              make_uint2(e4m3x4(f[k][0] * inv, f[k][1] * inv, f[k][2] * inv, f[k][3] * inv), e4m3x4(f[k][4] * inv, f[k][5] * inv, f[k][6] * inv, f[k][7] * inv));
+      }
+    } else {
+      const bool whole = tg * 4 >= lo && tg * 4 + 4 <= hi;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const uint32_t w = e4m3x4(f[0][i] * inv, f[1][i] * inv, f[2][i] * inv, f[3][i] * inv);
+        uint8_t *p = dst + (dg * 8 + i) * kBlk + tg * 4;
+        if (whole) *reinterpret_cast<uint32_t *>(p) = w;
+        else {
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            if (tg * 4 + k >= lo && tg * 4 + k < hi) p[k] = (uint8_t)(w >> (8 * k));
+        }
+      }
+    }
+  }
+  if (t == 0) a.scales[part] = scale;
+}
+
+}  // namespace
+
+extern "C" pd_status pd_cache_append(int32_t dtype, int32_t batch, int32_t n_kv_heads, int32_t n_blocks, int32_t max_blocks, int32_t rows,
+                                     int32_t max_new, const void *k, int64_t k_stride, const void *v, int64_t v_stride,
+                                     const int32_t *row_start, const int32_t *n_new, const int32_t *pos_start, const int32_t *table,
+                                     void *codes, float *scales, int32_t *status, void *cuda_stream) {
+  if (dtype != PD_DTYPE_FP32 && dtype != PD_DTYPE_BF16) return PD_ERR_ARG;
+  if (batch < 1 || batch > 65535 || n_kv_heads < 1 || n_kv_heads > 65535 || n_blocks < 1 || max_blocks < 1 || rows < 0 || max_new < 0) return PD_ERR_ARG;
+  if (max_new == 0 || rows == 0) return PD_OK;
+  if (!k || !v || !row_start || !n_new || !pos_start || !table || !codes || !scales) return PD_ERR_ARG;
+  const int e = dtype == PD_DTYPE_BF16 ? 2 : 4;
+  if (k_stride < (int64_t)n_kv_heads * kDh || v_stride < (int64_t)n_kv_heads * kDh || (k_stride * e) % 16 != 0 || (v_stride * e) % 16 != 0) return PD_ERR_ARG;
+  if ((reinterpret_cast<uintptr_t>(k) | reinterpret_cast<uintptr_t>(v) | reinterpret_cast<uintptr_t>(codes)) % 16 != 0 ||
+      reinterpret_cast<uintptr_t>(scales) % 8 != 0) return PD_ERR_ARG;
+  AppendArgs a;
+  a.heads = n_kv_heads; a.n_blocks = n_blocks; a.max_blocks = max_blocks; a.rows = rows; a.max_new = max_new;
+  a.k = k; a.v = v; a.k_stride = k_stride; a.v_stride = v_stride;
+  a.row_start = row_start; a.n_new = n_new; a.pos_start = pos_start; a.table = table;
+  a.codes = static_cast<uint8_t *>(codes); a.scales = scales; a.status = status;
+  // blocks that max_new tokens touch at most, wherever they begin
+  const dim3 grid((unsigned)(((long long)max_new + kBlk - 2) / kBlk + 1), n_kv_heads, batch);
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(cuda_stream);
+  if (dtype == PD_DTYPE_BF16) cache_append_kernel<__nv_bfloat16><<<grid, 256, 0, s>>>(a);
+  else cache_append_kernel<float><<<grid, 256, 0, s>>>(a);
+  return cudaGetLastError() == cudaSuccess ? PD_OK : PD_ERR_CUDA;
+}

@@ -1,0 +1,169 @@
+// Rotary positions on caller-supplied heads, without a decoder handle: neighbouring dims or the two halves paired, the whole
+// head or its first rot_dim dims, frequencies of the caller's choice (pd_rotary_turns has the usual ones), either direction.
+//
+//   t = 2 pi frac(pos * turns[i]),   y_a = A (x_a cos t - x_b sin t),   y_b = A (x_a sin t + x_b cos t)
+//
+// A frequency is held as turns per position in 64 bits: the product with the position keeps its fraction of a turn to 2^-52 of
+// the product, so that position 10^6 is as exact as position 1, and sincospif gets an argument in [-1, 1].  Sine and cosine
+// belong to a (token, pair), not to a head: a CTA computes those of its tokens once into shared memory and then streams all
+// heads through it, 16 bytes per load.  One read and one write of every element: HBM-bound for prompts, one launch latency
+// for a decode step.
+#include <math.h>
+
+#include "pd_internal.h"
+
+using namespace pd;
+
+namespace {
+
+constexpr int kRotThreads = 256;
+constexpr int kRotMaxTokens = 8;         // tokens per CTA
+constexpr int kRotMaxHead = 256;
+
+struct RotaryArgs {
+  const void *x; void *out;
+  long long x_tok, x_head, o_tok, o_head;     // strides in elements
+  const int32_t *pos; const double *turns;
+  float amplitude;
+  int tokens, heads, dh, rot, inverse, copy_rest, tok_per_cta;
+};
+
+template <typename T> __device__ __forceinline__ float to_f(T v);
+template <> __device__ __forceinline__ float to_f(float v) { return v; }
+template <> __device__ __forceinline__ float to_f(__nv_bfloat16 v) { return __bfloat162float(v); }
+template <typename T> __device__ __forceinline__ T of_f(float v);
+template <> __device__ __forceinline__ float of_f(float v) { return v; }
+template <> __device__ __forceinline__ __nv_bfloat16 of_f(float v) { return __float2bfloat16_rn(v); }
+
+template <typename T, int N> struct alignas(sizeof(T) * N) Vec { T v[N]; };
+
+// VEC elements per access: 16 bytes, or 1 where the shape, the strides or the addresses do not allow it.
+template <typename T, bool INTERLEAVED, int VEC>
+__global__ void __launch_bounds__(kRotThreads) rotary_kernel(RotaryArgs a) {
+  __shared__ float2 cs[kRotMaxTokens * kRotMaxHead / 2];
+  const int half = a.rot / 2, tok0 = blockIdx.x * a.tok_per_cta;
+  const int nt = min(a.tok_per_cta, a.tokens - tok0);
+  for (int i = threadIdx.x; i < nt * half; i += kRotThreads) {
+    const double t = (double)a.pos[tok0 + i / half] * a.turns[i % half];
+    float s, c;
+    sincospif((float)(2.0 * (t - rint(t))), &s, &c);
+    cs[i] = make_float2(c * a.amplitude, (a.inverse ? -s : s) * a.amplitude);
+  }
+  __syncthreads();
+  using V = Vec<T, VEC>;
+  // items of a head: VEC pairs (halves) or VEC / 2 pairs (neighbours) each - one pair where VEC is 1 -, then the rest of the head
+  constexpr int PAIRS = VEC == 1 ? 1 : INTERLEAVED ? VEC / 2 : VEC;
+  const int turn_items = half / PAIRS, items = turn_items + (a.copy_rest ? (a.dh - a.rot) / VEC : 0);
+  const int per_tok = items * a.heads, total = nt * per_tok;
+#pragma unroll 4
+  for (int i = threadIdx.x; i < total; i += kRotThreads) {
+    const int tt = i / per_tok, r = i - tt * per_tok, h = r / items, c = r - h * items;
+    const T *x = static_cast<const T *>(a.x) + (tok0 + tt) * a.x_tok + h * a.x_head;
+    T *o = static_cast<T *>(a.out) + (tok0 + tt) * a.o_tok + h * a.o_head;
+    if (c >= turn_items) {
+      const int at = a.rot + (c - turn_items) * VEC;
+      *reinterpret_cast<V *>(o + at) = *reinterpret_cast<const V *>(x + at);
+      continue;
+    }
+    const float2 *w = cs + tt * half + c * PAIRS;
+    if (INTERLEAVED && VEC > 1) {
+      V p = *reinterpret_cast<const V *>(x + c * VEC);
+#pragma unroll
+      for (int k = 0; k < VEC / 2; ++k) {
+        const float xa = to_f(p.v[2 * k]), xb = to_f(p.v[2 * k + 1]);
+        p.v[2 * k] = of_f<T>(xa * w[k].x - xb * w[k].y);
+        p.v[2 * k + 1] = of_f<T>(xa * w[k].y + xb * w[k].x);
+      }
+      *reinterpret_cast<V *>(o + c * VEC) = p;
+    } else {
+      const int ia = INTERLEAVED ? 2 * c : c * VEC, ib = INTERLEAVED ? 2 * c + 1 : half + c * VEC;
+      V pa = *reinterpret_cast<const V *>(x + ia), pb = *reinterpret_cast<const V *>(x + ib);
+#pragma unroll
+      for (int k = 0; k < VEC; ++k) {
+        const float xa = to_f(pa.v[k]), xb = to_f(pb.v[k]);
+        pa.v[k] = of_f<T>(xa * w[k].x - xb * w[k].y);
+        pb.v[k] = of_f<T>(xa * w[k].y + xb * w[k].x);
+      }
+      *reinterpret_cast<V *>(o + ia) = pa;
+      *reinterpret_cast<V *>(o + ib) = pb;
+    }
+  }
+}
+
+template <typename T, int VEC>
+cudaError_t launch_rotary(const RotaryArgs &a, int interleaved, cudaStream_t s) {
+  const int grid = (a.tokens + a.tok_per_cta - 1) / a.tok_per_cta;
+  if (interleaved) rotary_kernel<T, true, VEC><<<grid, kRotThreads, 0, s>>>(a);
+  else rotary_kernel<T, false, VEC><<<grid, kRotThreads, 0, s>>>(a);
+  return cudaGetLastError();
+}
+
+}  // namespace
+
+extern "C" {
+
+pd_status pd_rotary_turns(int32_t rot_dim, double theta, int32_t scaling, double factor, int32_t original_len, double fast_turns,
+                          double slow_turns, double *turns, float *amplitude) {
+  if (!turns || rot_dim < 2 || rot_dim > kRotMaxHead || rot_dim % 2 || !(theta > 1.0) || !isfinite(theta)) return PD_ERR_ARG;
+  if (scaling != PD_ROTARY_PLAIN && scaling != PD_ROTARY_LINEAR && scaling != PD_ROTARY_BY_PARTS) return PD_ERR_ARG;
+  if (scaling != PD_ROTARY_PLAIN && (!(factor >= 1.0) || !isfinite(factor))) return PD_ERR_ARG;
+  const double two_pi = 6.283185307179586476925;
+  double lo = 0.0, hi = 0.0;
+  if (scaling == PD_ROTARY_BY_PARTS) {
+    if (original_len < 1 || !(slow_turns > 0.0) || !(fast_turns >= slow_turns) || !isfinite(fast_turns)) return PD_ERR_ARG;
+    // pair index (of rot_dim / 2, as a real number) that makes `n` turns over the original context: theta^(-2 i / rot) L / (2 pi) = n
+    auto pair_of = [&](double n) { return rot_dim * log(original_len / (n * two_pi)) / (2.0 * log(theta)); };
+    lo = fmax(floor(pair_of(fast_turns)), 0.0);
+    hi = fmin(ceil(pair_of(slow_turns)), rot_dim - 1.0);
+  }
+  for (int i = 0; i < rot_dim / 2; ++i) {
+    double f = pow(theta, -2.0 * i / rot_dim);
+    if (scaling == PD_ROTARY_LINEAR) f /= factor;
+    if (scaling == PD_ROTARY_BY_PARTS) {
+      const double ramp = fmin(fmax((i - lo) / fmax(hi - lo, 1e-3), 0.0), 1.0);
+      f = f / factor * ramp + f * (1.0 - ramp);
+    }
+    turns[i] = f / two_pi;
+  }
+  if (amplitude) *amplitude = scaling == PD_ROTARY_BY_PARTS ? (float)(0.1 * log(factor) + 1.0) : 1.f;
+  return PD_OK;
+}
+
+pd_status pd_rotary(int32_t dtype, int32_t tokens, int32_t n_heads, int32_t d_head, int32_t rot_dim, int32_t interleaved, int32_t inverse,
+                    const void *x, int64_t x_token_stride, int64_t x_head_stride, const int32_t *positions, const double *turns,
+                    float amplitude, void *out, int64_t out_token_stride, int64_t out_head_stride, void *cuda_stream) {
+  if (dtype != PD_DTYPE_FP32 && dtype != PD_DTYPE_BF16) return PD_ERR_ARG;
+  if (tokens < 0 || n_heads < 1 || n_heads > 65535 || d_head < 2 || d_head > kRotMaxHead) return PD_ERR_ARG;
+  if (rot_dim < 2 || rot_dim > d_head || rot_dim % 2) return PD_ERR_ARG;
+  if (x_token_stride < 0 || x_head_stride < 0 || out_token_stride < 0 || out_head_stride < 0) return PD_ERR_ARG;
+  if (tokens == 0) return PD_OK;
+  if (!x || !positions || !turns || !out) return PD_ERR_ARG;
+  const size_t e = dtype == PD_DTYPE_BF16 ? 2 : 4;
+  if ((reinterpret_cast<uintptr_t>(x) | reinterpret_cast<uintptr_t>(out)) % e != 0 || reinterpret_cast<uintptr_t>(positions) % 4 != 0 ||
+      reinterpret_cast<uintptr_t>(turns) % 8 != 0) return PD_ERR_ARG;
+  // the output's heads must not overlap: heads inside tokens, or tokens inside heads
+  const bool by_token = (n_heads == 1 || out_head_stride >= d_head) && (tokens == 1 || out_token_stride >= (n_heads - 1) * out_head_stride + d_head);
+  const bool by_head = (tokens == 1 || out_token_stride >= d_head) && (n_heads == 1 || out_head_stride >= (tokens - 1) * out_token_stride + d_head);
+  if (!by_token && !by_head) return PD_ERR_ARG;
+  const bool in_place = x == out;
+  if (in_place && (x_token_stride != out_token_stride || x_head_stride != out_head_stride)) return PD_ERR_ARG;
+  RotaryArgs a;
+  a.x = x; a.out = out;
+  a.x_tok = x_token_stride; a.x_head = x_head_stride; a.o_tok = out_token_stride; a.o_head = out_head_stride;
+  a.pos = positions; a.turns = turns; a.amplitude = amplitude;
+  a.tokens = tokens; a.heads = n_heads; a.dh = d_head; a.rot = rot_dim; a.inverse = inverse != 0;
+  a.copy_rest = !in_place && rot_dim < d_head;
+  // as many tokens per CTA as leave four CTAs per SM
+  a.tok_per_cta = max(1, min(kRotMaxTokens, tokens / (4 * kSms)));
+  const int vec = (int)(16 / e);
+  const bool wide = (reinterpret_cast<uintptr_t>(x) | reinterpret_cast<uintptr_t>(out)) % 16 == 0 &&
+                    (x_token_stride | x_head_stride | out_token_stride | out_head_stride) % vec == 0 &&
+                    (interleaved ? rot_dim : rot_dim / 2) % vec == 0 && d_head % vec == 0;
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(cuda_stream);
+  cudaError_t st;
+  if (dtype == PD_DTYPE_BF16) st = wide ? launch_rotary<__nv_bfloat16, 8>(a, interleaved, s) : launch_rotary<__nv_bfloat16, 1>(a, interleaved, s);
+  else st = wide ? launch_rotary<float, 4>(a, interleaved, s) : launch_rotary<float, 1>(a, interleaved, s);
+  return st == cudaSuccess ? PD_OK : PD_ERR_CUDA;
+}
+
+}  // extern "C"
