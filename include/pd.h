@@ -472,7 +472,7 @@ PD_API pd_status pd_cache_append(int32_t dtype, int32_t batch, int32_t n_kv_head
  * begin <= p < end of sequence b that hold tokens (p < lens[b]):
  *   score = attn_scale * q . k_p;  softcap > 0: softcap * tanh(score / softcap);  bias: + bias[head][min(end - 1 - p, n_bias - 1)]
  *   out   = softmax over those p of score . v
- * and is zero where it sees nothing; rows at or beyond n_rows[b] are not read and come back as zeros.  Query head h reads
+ * and is zero where it sees nothing; rows at or beyond n_rows[b] may hold anything and come back as zeros.  Query head h reads
  * key head h / (n_heads / n_kv_heads).
  *   dtype      PD_DTYPE_FP32 or PD_DTYPE_BF16: element type of q and out.  bf16: scores and sums in fp32, weights rounded to f16 (11 bits);
  *              fp32: queries and weights in two f16 parts (22 bits)

@@ -6,6 +6,7 @@ There is no fallback: if libpd.so is missing or does not load, importing this mo
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 from typing import Dict, Optional, Sequence
 
@@ -519,29 +520,41 @@ def linear(a, w, mode: int = 0, row_sumsq=None, eps: float = 1e-6, x=None, gain_
     return out
 
 
-def _stream_of(t) -> int:
-    """The current stream of a tensor's device, which becomes the current device of this thread's call."""
-    import torch
-    if not t.is_cuda:
+# The operators below take a few microseconds on the device, so their checks are kept to what an attribute look-up costs.
+class _Torch:
+    """torch's types and current stream, looked up at the first use (importing this module does not import torch)."""
+    pd_dtype = None
+
+    @classmethod
+    def load(cls):
+        import torch
+        cls.float32, cls.float64, cls.int32, cls.uint8 = torch.float32, torch.float64, torch.int32, torch.uint8
+        cls.current_device = staticmethod(torch.cuda.current_device)
+        # the raw handle of a device's current stream; torch.cuda.current_stream builds an object around it (2 us)
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        cls.stream = staticmethod(raw if raw is not None else lambda d: torch.cuda.current_stream(d).cuda_stream)
+        cls.pd_dtype = {torch.bfloat16: PD_DTYPE_BF16, torch.float32: PD_DTYPE_FP32}
+
+
+def _op_start(t):
+    """(pd dtype, device ordinal, current stream) for a call whose main tensor is t."""
+    if _Torch.pd_dtype is None:
+        _Torch.load()
+    dt = _Torch.pd_dtype.get(t.dtype)
+    if dt is None:
+        raise ValueError(f"expected float32 or bfloat16, got {t.dtype}")
+    dev = t.get_device()
+    if dev < 0:
         raise ValueError("tensors must be CUDA tensors")
-    if t.device.index != torch.cuda.current_device():
-        raise ValueError(f"tensors are on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
-    return torch.cuda.current_stream(t.device).cuda_stream
+    if dev != _Torch.current_device():
+        raise ValueError(f"tensors are on cuda:{dev}, the current device is cuda:{_Torch.current_device()}")
+    return dt, dev, _Torch.stream(dev)
 
 
-def _dtype_of(t) -> int:
-    import torch
-    if t.dtype == torch.bfloat16:
-        return PD_DTYPE_BF16
-    if t.dtype == torch.float32:
-        return PD_DTYPE_FP32
-    raise ValueError(f"expected float32 or bfloat16, got {t.dtype}")
-
-
-def _plain(what: str, t, like, dtype, shape):
-    """A contiguous tensor of this type and shape on the device of `like`, or ValueError."""
-    if t.dtype != dtype or t.shape != shape or t.device != like.device or not t.is_contiguous():
-        raise ValueError(f"{what} must be a contiguous {dtype} tensor of shape {tuple(shape)} on {like.device}")
+def _plain(what: str, t, dev: int, dtype, shape):
+    """The address of a contiguous tensor of this type and shape on device `dev`, or ValueError."""
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != dev or not t.is_contiguous():
+        raise ValueError(f"{what} must be a contiguous {dtype} tensor of shape {tuple(shape)} on cuda:{dev}")
     return t.data_ptr()
 
 
@@ -560,60 +573,65 @@ def rotary_turns(rot_dim: int, theta: float = 10000.0, scaling: int = PD_ROTARY_
 def rotary(x, positions, turns, amplitude: float = 1.0, interleaved: bool = False, inverse: bool = False, out=None):
     """pd_rotary on torch CUDA tensors: x [tokens, heads, d_head] bfloat16 or float32 (any token and head stride), positions int32
     [tokens], turns float64 [rot_dim / 2].  Returns `out` (allocated here when not given; x itself rotates in place).  Runs on
-    torch's current stream."""
-    import torch
-    dt = _dtype_of(x)
-    if x.dim() != 3 or x.stride(2) != 1 and x.shape[2] > 1:
-        raise ValueError("x must be [tokens, heads, d_head] with neighbouring dims")
-    n, heads, dh = x.shape
+    torch's current stream of the current device, where all tensors are."""
+    dt, dev, stream = _op_start(x)
+    if x.dim() != 3 or turns.dim() != 1:
+        raise ValueError("x must be [tokens, heads, d_head], turns [rot_dim / 2]")
+    n, heads, dh = shape = x.shape
+    xt, xh, one = x.stride()
     if out is None:
-        out = torch.empty((n, heads, dh), dtype=x.dtype, device=x.device)
-    elif out.shape != x.shape or out.dtype != x.dtype or out.device != x.device or out.stride(2) != 1:
-        raise ValueError("out must have x's shape, type and device, with neighbouring dims")
-    if turns.dim() != 1:
-        raise ValueError("turns must be [rot_dim / 2]")
-    pos = _plain("positions", positions, x, torch.int32, (n,))
-    tr = _plain("turns", turns, x, torch.float64, turns.shape)
-    st = _lib.pd_rotary(dt, n, heads, dh, 2 * turns.shape[0], interleaved, inverse, x.data_ptr(), x.stride(0), x.stride(1), pos, tr, amplitude,
-                        out.data_ptr(), out.stride(0), out.stride(1), _stream_of(x))
+        out = x.new_empty(shape)
+    elif out.shape != shape or out.dtype is not x.dtype or out.get_device() != dev:
+        raise ValueError("out must have x's shape, type and device")
+    ot, oh, o_one = out.stride()
+    if (one != 1 or o_one != 1) and dh > 1:
+        raise ValueError("the dims of a head must be neighbours")
+    half = turns.shape[0]
+    st = _lib.pd_rotary(dt, n, heads, dh, 2 * half, interleaved, inverse, x.data_ptr(), xt, xh, _plain("positions", positions, dev, _Torch.int32, (n,)),
+                        _plain("turns", turns, dev, _Torch.float64, (half,)), amplitude, out.data_ptr(), ot, oh, stream)
     if st != PD_OK:
         raise PdError(st, "pd_rotary")
     return out
 
 
-def _cache_args(codes, scales, table, like):
-    """(n_blocks, kv heads, max_blocks, pointers) of an 8-bit paged cache."""
-    import torch
+def _cache_args(codes, scales, table, dev: int):
+    """(n_blocks, kv heads, batch, max_blocks, pointers) of an 8-bit paged cache."""
     if codes.dim() != 4 or table.dim() != 2:
         raise ValueError("codes must be [blocks, kv heads, 2, 4096], table [batch, blocks of a sequence]")
     n_blocks, heads = codes.shape[:2]
-    return (n_blocks, heads, table.shape[1], _plain("codes", codes, like, torch.uint8, (n_blocks, heads, 2, PD_CACHE_BLOCK * 64)),
-            _plain("scales", scales, like, torch.float32, (n_blocks, heads, 2)), _plain("table", table, like, torch.int32, table.shape))
+    batch, max_blocks = table.shape
+    return (n_blocks, heads, batch, max_blocks, _plain("codes", codes, dev, _Torch.uint8, (n_blocks, heads, 2, PD_CACHE_BLOCK * 64)),
+            _plain("scales", scales, dev, _Torch.float32, (n_blocks, heads, 2)), _plain("table", table, dev, _Torch.int32, (batch, max_blocks)))
 
 
 def cache_append(k, v, row_start, n_new, pos_start, table, codes, scales, max_new: int, status=None):
     """pd_cache_append on torch CUDA tensors: k, v [rows, kv heads, 64] bfloat16 or float32 (any row stride), row_start, n_new, pos_start
     int32 [batch], table int32 [batch, blocks], codes uint8 [blocks, kv heads, 2, 4096] and scales float32 [blocks, kv heads, 2],
-    both written in place; max_new: host bound on n_new; status: int32 [1] or None.  Runs on torch's current stream."""
-    import torch
-    dt = _dtype_of(k)
-    n_blocks, heads, max_blocks, cp, sp, tp = _cache_args(codes, scales, table, k)
-    rows, batch = k.shape[0], table.shape[0]
+    both written in place; max_new: host bound on n_new; status: int32 [1] or None.  Runs on torch's current stream of the
+    current device, where all tensors are."""
+    dt, dev, stream = _op_start(k)
+    n_blocks, heads, batch, max_blocks, cp, sp, tp = _cache_args(codes, scales, table, dev)
+    rows = k.shape[0]
+    strides = []
     for t in (k, v):
-        if t.shape != (rows, heads, 64) or t.dtype != k.dtype or t.device != k.device or t.stride(2) != 1 or (heads > 1 and t.stride(1) != 64):
-            raise ValueError("k and v must be [rows, kv heads, 64] of one type, with neighbouring heads and dims")
-    i32 = torch.int32
-    one = heads * 64
-    st = _lib.pd_cache_append(dt, batch, heads, n_blocks, max_blocks, rows, max_new, k.data_ptr(), k.stride(0) if rows > 1 else one, v.data_ptr(),
-                              v.stride(0) if rows > 1 else one,
-                              _plain("row_start", row_start, k, i32, (batch,)), _plain("n_new", n_new, k, i32, (batch,)),
-                              _plain("pos_start", pos_start, k, i32, (batch,)), tp, cp, sp,
-                              None if status is None else _plain("status", status, k, i32, (1,)), _stream_of(k))
+        if t.shape != (rows, heads, 64) or t.dtype is not k.dtype or t.get_device() != dev:
+            raise ValueError("k and v must be [rows, kv heads, 64], of one type and device")
+        s = t.stride()
+        if s[2] != 1 or (heads > 1 and s[1] != 64):
+            raise ValueError("the heads of a row of k and v, and their dims, must be neighbours")
+        strides.append(s[0] if rows > 1 else heads * 64)                               # a dimension of one has any stride
+    i32, per = _Torch.int32, (batch,)
+    st = _lib.pd_cache_append(dt, batch, heads, n_blocks, max_blocks, rows, max_new, k.data_ptr(), strides[0], v.data_ptr(), strides[1],
+                              _plain("row_start", row_start, dev, i32, per), _plain("n_new", n_new, dev, i32, per),
+                              _plain("pos_start", pos_start, dev, i32, per), tp, cp, sp,
+                              None if status is None else _plain("status", status, dev, i32, (1,)), stream)
     if st != PD_OK:
         raise PdError(st, "pd_cache_append")
 
 
+@functools.lru_cache(maxsize=256)
 def cache_attention_scratch_bytes(dtype: int, batch: int, rows_per_seq: int, n_heads: int, n_kv_heads: int, max_len: int) -> int:
+    """pd_cache_attention_scratch_bytes: a function of sizes alone (0: a size out of range)."""
     return int(_lib.pd_cache_attention_scratch_bytes(dtype, batch, rows_per_seq, n_heads, n_kv_heads, max_len))
 
 
@@ -622,37 +640,45 @@ def cache_attention(q, codes, scales, table, n_rows, lens, attn_scale: float, ma
     """pd_cache_attention on torch CUDA tensors: q [batch, rows, heads * 64] bfloat16 or float32 (any row stride, batches rows apart),
     the cache as in cache_append, n_rows and lens int32 [batch], spans int32 [batch, rows, 2] or None, bias float32 [heads, n] or
     None; max_len: host bound on lens (the table's extent when not given).  `out` [batch, rows, heads * 64] and `scratch`
-    (uint8, 16-byte aligned) are allocated here when not given.  Runs on torch's current stream; returns out."""
-    import torch
-    dt = _dtype_of(q)
-    n_blocks, kv_heads, max_blocks, cp, sp, tp = _cache_args(codes, scales, table, q)
-    if q.dim() != 3 or q.shape[2] % 64 or q.stride(2) != 1 or table.shape[0] != q.shape[0]:
+    (16-byte aligned) are allocated here when not given.  Runs on torch's current stream of the current device, where all
+    tensors are; returns out."""
+    dt, dev, stream = _op_start(q)
+    n_blocks, kv_heads, t_batch, max_blocks, cp, sp, tp = _cache_args(codes, scales, table, dev)
+    if q.dim() != 3:
+        raise ValueError("q must be [batch, rows, heads * 64]")
+    batch, rows, width = shape = q.shape
+    qb, qr, one = q.stride()
+    if width % 64 or (one != 1 and width > 1) or t_batch != batch:
         raise ValueError("q must be [batch, rows, heads * 64] with neighbouring dims, for the table's batch")
-    batch, rows, width = q.shape
-    stride = q.stride(1) if rows > 1 else q.stride(0) if batch > 1 else width       # a dimension of one has any stride
-    if batch > 1 and q.stride(0) != rows * stride:
+    stride = qr if rows > 1 else qb if batch > 1 else width                            # a dimension of one has any stride
+    if batch > 1 and qb != rows * stride:
         raise ValueError("q's batches must lie rows apart")
-    heads = width // 64
+    heads, i32, per = width // 64, _Torch.int32, (batch,)
     if max_len is None:
         max_len = min(max_blocks * PD_CACHE_BLOCK, (1 << 31) - 1 - PD_CACHE_BLOCK)
-    i32 = torch.int32
     if out is None:
-        out = torch.empty((batch, rows, width), dtype=q.dtype, device=q.device)
+        out = q.new_empty(shape)
         op = out.data_ptr()
     else:
-        op = _plain("out", out, q, q.dtype, (batch, rows, width))
+        op = _plain("out", out, dev, q.dtype, shape)
     if scratch is None:
-        scratch = torch.empty(_lib.pd_cache_attention_scratch_bytes(dt, batch, rows, heads, kv_heads, max_len), dtype=torch.uint8, device=q.device)
-    elif scratch.device != q.device or not scratch.is_contiguous():
-        raise ValueError("scratch must be contiguous, on q's device")
-    if bias is not None and bias.dim() != 2:
-        raise ValueError("bias must be [heads, distances]")
+        n_scratch = cache_attention_scratch_bytes(dt, batch, rows, heads, kv_heads, max_len)
+        scratch = q.new_empty((n_scratch,), dtype=_Torch.uint8) if n_scratch > 256 else None      # 256: no partial results
+        scratch_ptr = None if scratch is None else scratch.data_ptr()
+    else:
+        if scratch.get_device() != dev or not scratch.is_contiguous():
+            raise ValueError("scratch must be contiguous, on q's device")
+        n_scratch, scratch_ptr = scratch.numel() * scratch.element_size(), scratch.data_ptr()
+    bias_ptr, n_bias = None, 0
+    if bias is not None:
+        if bias.dim() != 2:
+            raise ValueError("bias must be [heads, distances]")
+        n_bias = bias.shape[1]
+        bias_ptr = _plain("bias", bias, dev, _Torch.float32, (heads, n_bias))
     st = _lib.pd_cache_attention(dt, batch, rows, heads, kv_heads, n_blocks, max_blocks, max_len, attn_scale, softcap, q.data_ptr(), stride, cp, sp, tp,
-                                 _plain("n_rows", n_rows, q, i32, (batch,)), _plain("lens", lens, q, i32, (batch,)),
-                                 None if spans is None else _plain("spans", spans, q, i32, (batch, rows, 2)),
-                                 None if bias is None else _plain("bias", bias, q, torch.float32, (heads, bias.shape[1])),
-                                 0 if bias is None else bias.shape[1], op, scratch.data_ptr(), scratch.numel() * scratch.element_size(),
-                                 None if status is None else _plain("status", status, q, i32, (1,)), _stream_of(q))
+                                 _plain("n_rows", n_rows, dev, i32, per), _plain("lens", lens, dev, i32, per),
+                                 None if spans is None else _plain("spans", spans, dev, i32, (batch, rows, 2)), bias_ptr, n_bias, op, scratch_ptr, n_scratch,
+                                 None if status is None else _plain("status", status, dev, i32, (1,)), stream)
     if st != PD_OK:
         raise PdError(st, "pd_cache_attention")
     return out

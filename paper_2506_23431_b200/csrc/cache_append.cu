@@ -14,6 +14,7 @@
 // writes keys as 8 bytes per token and values, whose layout is turned, as whole words of four tokens, with no pass through shared memory.
 #include <cuda_fp16.h>
 
+#include "op_launch.cuh"
 #include "pd_internal.h"
 
 using namespace pd;
@@ -70,6 +71,7 @@ __device__ __forceinline__ void load8(const __nv_bfloat16 *p, float (&f)[8]) {
 
 template <typename T>
 __global__ void __launch_bounds__(256) cache_append_kernel(AppendArgs a) {
+  op_begin();
   const int b = blockIdx.z, h = blockIdx.y, is_v = threadIdx.x >> 7, t = threadIdx.x & 127;
   const long long n = a.n_new[b], p0 = a.pos_start[b], row0 = a.row_start[b];
   if (n <= 0) return;
@@ -183,7 +185,6 @@ extern "C" pd_status pd_cache_append(int32_t dtype, int32_t batch, int32_t n_kv_
   // blocks that max_new tokens touch at most, wherever they begin
   const dim3 grid((unsigned)(((long long)max_new + kBlk - 2) / kBlk + 1), n_kv_heads, batch);
   cudaStream_t s = reinterpret_cast<cudaStream_t>(cuda_stream);
-  if (dtype == PD_DTYPE_BF16) cache_append_kernel<__nv_bfloat16><<<grid, 256, 0, s>>>(a);
-  else cache_append_kernel<float><<<grid, 256, 0, s>>>(a);
-  return cudaGetLastError() == cudaSuccess ? PD_OK : PD_ERR_CUDA;
+  const cudaError_t st = op_launch(dtype == PD_DTYPE_BF16 ? cache_append_kernel<__nv_bfloat16> : cache_append_kernel<float>, grid, 256, 0, 1, s, a);
+  return st == cudaSuccess ? PD_OK : PD_ERR_CUDA;
 }

@@ -16,10 +16,12 @@
 // the largest in f16, the block's sum of values is a fresh accumulator, and only then do the running maximum and the values' scale come in, in 32 bits - a
 // block of tiny weights and large values loses nothing.  32-bit queries and weights go through two f16 parts (22 bits).
 #include <cuda_fp16.h>
+#include <float.h>
 #include <limits.h>
 
 #include <algorithm>
 
+#include "op_launch.cuh"
 #include "pd_internal.h"
 
 using namespace pd;
@@ -28,18 +30,28 @@ namespace {
 
 constexpr int kBlk = PD_CACHE_BLOCK;
 constexpr int kPart = kBlk * kDh;                 // codes of a block's keys (values) of one head
-constexpr int kStageBytes = 2 * kPart;
 constexpr int kWarps = 4, kThreads = kWarps * 32;
-constexpr int kStages = 3;
-constexpr int kRingBytes = kWarps * kStages * kStageBytes;
-constexpr int kSmem = kRingBytes + kWarps * kStages * 8;
-constexpr int kCtasPerSm = 2;
+constexpr int kMaxCluster = 8, kClusterSms = 128;
+constexpr int kOuterBlocks = 4;                   // fewest blocks for each warp where a segment is split beyond a cluster
+// CTAs per SM as the registers allow (one 16-row tile 128, two f16 parts 168, two tiles 255), and slots of 4 KB (a block's keys, or its values) in
+// a warp's ring: what then fits the shared memory.
+__host__ __device__ constexpr int ctas_per_sm(int mt, bool f32) { return mt == 2 ? 2 : f32 ? 3 : 4; }
+__host__ __device__ constexpr int slots(int mt, bool f32) { return mt == 2 ? 6 : f32 ? 4 : 3; }
+__host__ __device__ constexpr int ring_bytes(int mt, bool f32) { return kWarps * slots(mt, f32) * kPart; }
+constexpr int kRec = kDh + 4;                     // a row's partial result: 64 sums, maximum, sum of weights, alignment
+__host__ __device__ constexpr int inbox_bytes(int mt) { return mt * 16 * kRec * (int)sizeof(float); }
+// What a warp looks up rather than holds in registers: scales and ids of two runs of 16 blocks, spans of its rows, its ring's barriers.
+constexpr int kRun = 16;
+template <int MT> struct WarpNotes { float2 scale[2 * kRun]; int id[2 * kRun]; int2 span[MT * 16]; uint64_t bar[8]; };
+__host__ __device__ constexpr int smem_bytes(int mt, bool f32) {
+  return ring_bytes(mt, f32) + inbox_bytes(mt) + kWarps * (int)(mt == 2 ? sizeof(WarpNotes<2>) : sizeof(WarpNotes<1>));
+}
 constexpr uint32_t kSpinLimit = 1u << 24;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLift = 15.f;                     // weights are 2^(s - max + kLift): at most 2^15 in f16
 
 struct CacheAttnArgs {
-  int R, H, HK, G, n_blocks, max_blocks, max_len, tiles, splits, n_bias;
+  int R, H, HK, G, n_blocks, max_blocks, max_len, tiles, cluster, outer, n_bias;
   float scale_log2e, cap_log2e, inv_cap;          // cap_log2e = 0: no cap; inv_cap = 2 * scale / cap * log2(e) (bf16) or scale / cap (fp32)
   const void *q; long long q_row;                 // row b * R + r of the queries at (b * R + r) * q_row
   const uint8_t *codes; const float2 *scales; const int32_t *table, *n_rows, *lens; const int2 *spans; const float *bias;
@@ -56,8 +68,16 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity) {      
   return false;
 }
 __device__ __forceinline__ void fetch(uint32_t dst, const uint8_t *src, uint32_t bar) {
-  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(kStageBytes) : "memory");
-  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(kStageBytes), "r"(bar) : "memory");
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(kPart) : "memory");
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(kPart), "r"(bar) : "memory");
+}
+template <typename V>
+__device__ __forceinline__ void async_copy(V *dst, const V *src) {                 // 4 or 8 bytes into shared memory, through no register
+  asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(smem_u32(dst)), "l"(src), "n"(sizeof(V)) : "memory");
+}
+__device__ __forceinline__ void async_copies_land() {                              // the warp's copies are visible to all its lanes
+  asm volatile("cp.async.wait_all;" ::: "memory");
+  __syncwarp();
 }
 __device__ __forceinline__ uint4 lds128(uint32_t a) {
   uint4 v;
@@ -68,9 +88,12 @@ __device__ __forceinline__ void mma_f16(float (&c)[4], const uint32_t (&a)[4], u
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
+__device__ __forceinline__ void mma_f16_first(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {      // onto zero
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+               : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
+}
 __device__ __forceinline__ void widen(uint32_t w, uint32_t &lo, uint32_t &hi) {    // four codes -> two f16 pairs
-  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(lo) : "h"((unsigned short)(w & 0xffffu)));
-  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(hi) : "h"((unsigned short)(w >> 16)));
+  asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, a;\n\tcvt.rn.f16x2.e4m3x2 %1, b;\n\t}" : "=r"(lo), "=r"(hi) : "r"(w));
 }
 __device__ __forceinline__ uint32_t pack(float lo, float hi) {
   const __half2 v = __floats2half2_rn(lo, hi);
@@ -90,25 +113,35 @@ __device__ __forceinline__ float quad_max(float v) {
   v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 1));
   return fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 2));
 }
-__device__ __forceinline__ float quad_sum(float v) {
-  v += __shfl_xor_sync(0xffffffffu, v, 1);
-  return v + __shfl_xor_sync(0xffffffffu, v, 2);
+__device__ __forceinline__ uint32_t peer_addr(uint32_t addr, int rank) {           // the same place of another CTA of the cluster
+  uint32_t at;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(addr), "r"(rank));
+  return at;
 }
+__device__ __forceinline__ void peer_st4(uint32_t at, float4 v) {
+  asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(at), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w) : "memory");
+}
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 // bytes of a word that hold the code of "no number" (0x7f, 0xff), as 0x80 each
 __device__ __forceinline__ uint32_t nan_bytes(uint32_t w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
 
-__device__ __forceinline__ void load16(const float *p, float (&f)[16]) {
+// the first n bytes of a word
+__device__ __forceinline__ uint32_t below(int n) { return n >= 4 ? 0xffffffffu : n <= 0 ? 0u : (1u << (8 * n)) - 1; }
+
+// Sixteen dims of a row as they lie in memory, and as numbers.
+template <typename T> struct Raw16 { uint4 v[sizeof(T)]; };
+__device__ __forceinline__ void unpack16(const Raw16<float> &r, float (&f)[16]) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const float4 v = reinterpret_cast<const float4 *>(p)[i];
-    f[4 * i] = v.x; f[4 * i + 1] = v.y; f[4 * i + 2] = v.z; f[4 * i + 3] = v.w;
+    f[4 * i] = __uint_as_float(r.v[i].x); f[4 * i + 1] = __uint_as_float(r.v[i].y);
+    f[4 * i + 2] = __uint_as_float(r.v[i].z); f[4 * i + 3] = __uint_as_float(r.v[i].w);
   }
 }
-__device__ __forceinline__ void load16(const __nv_bfloat16 *p, float (&f)[16]) {
+__device__ __forceinline__ void unpack16(const Raw16<__nv_bfloat16> &r, float (&f)[16]) {
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
-    const uint4 v = reinterpret_cast<const uint4 *>(p)[i];
-    const uint32_t u[4] = {v.x, v.y, v.z, v.w};
+    const uint32_t u[4] = {r.v[i].x, r.v[i].y, r.v[i].z, r.v[i].w};
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       f[8 * i + 2 * k] = __uint_as_float(u[k] << 16);
@@ -116,76 +149,100 @@ __device__ __forceinline__ void load16(const __nv_bfloat16 *p, float (&f)[16]) {
     }
   }
 }
+__device__ __forceinline__ void store4(float *p, float4 v) { *reinterpret_cast<float4 *>(p) = v; }
+__device__ __forceinline__ void store4(__nv_bfloat16 *p, float4 v) {
+  const __nv_bfloat162 a = __floats2bfloat162_rn(v.x, v.y), b = __floats2bfloat162_rn(v.z, v.w);
+  *reinterpret_cast<uint2 *>(p) = make_uint2(*reinterpret_cast<const uint32_t *>(&a), *reinterpret_cast<const uint32_t *>(&b));
+}
 __device__ __forceinline__ void store2(float *p, float a, float b) { *reinterpret_cast<float2 *>(p) = make_float2(a, b); }
 __device__ __forceinline__ void store2(__nv_bfloat16 *p, float a, float b) { *reinterpret_cast<__nv_bfloat162 *>(p) = __floats2bfloat162_rn(a, b); }
 
-// One row of the tile that this lane holds columns of: what it sees, and its softmax so far.
+// One row of the tile that this lane holds columns of: its softmax so far.
 struct Row {
-  int begin, end;                   // visible positions; begin == end: none
   float mul;                        // score in log2 units (or the cap's argument) per unit of q . code at a key scale of 1
   float m, l;
-  const float *bias;                // the head's
 };
 
 // T: type of queries and output; MT: 16-row tiles; MOD: cap or bias.  fp32: queries and weights in two f16 parts.
 template <typename T, int MT, bool MOD>
-__global__ void __launch_bounds__(kThreads, kCtasPerSm) cache_attn_kernel(CacheAttnArgs a) {
-  constexpr int NP = sizeof(T) == 4 ? 2 : 1;
+__global__ void __launch_bounds__(kThreads, ctas_per_sm(MT, sizeof(T) == 4)) cache_attn_kernel(CacheAttnArgs a) {
+  constexpr int NP = sizeof(T) == 4 ? 2 : 1, NS = slots(MT, NP == 2), RING = ring_bytes(MT, NP == 2);
   constexpr int ROWS = MT * 16;
   extern __shared__ __align__(128) uint8_t ring[];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-  const int split = blockIdx.x, kvh = blockIdx.y / a.tiles, tile = blockIdx.y % a.tiles, b = blockIdx.z;
-  const uint32_t stage0 = smem_u32(ring) + warp * kStages * kStageBytes, bar0 = smem_u32(ring) + kRingBytes + warp * kStages * 8;
+  const int split = blockIdx.x, splits = gridDim.x, kvh = blockIdx.y / a.tiles, tile = blockIdx.y % a.tiles, b = blockIdx.z;
+  WarpNotes<MT> &notes = reinterpret_cast<WarpNotes<MT> *>(ring + RING + inbox_bytes(MT))[warp];
+  const uint32_t slot0 = smem_u32(ring) + warp * NS * kPart, bar0 = smem_u32(notes.bar);
   if (lane == 0) {
-    for (int s = 0; s < kStages; ++s) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(bar0 + s * 8) : "memory");
+    for (int s = 0; s < NS; ++s) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(bar0 + s * 8) : "memory");
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   __syncwarp();
+  if (a.cluster > 1) cluster_arrive();             // waited for where the first CTA writes into another
+  op_begin();
+
+  // ---- one round of independent loads: counts, the table where the blocks are if the sequence has its full length, spans, queries
+  const int blocks_most = (int)min(((long long)a.max_len + kBlk - 1) / kBlk, (long long)a.max_blocks);
+  const int32_t *table = a.table + (size_t)b * a.max_blocks;
+  // this CTA's share of n blocks: the first n % splits CTAs have one more
+  auto share = [&](int n, int k) { const int q = n / splits; return q * k + min(k, n - q * splits); };
+  const int guess = share(blocks_most, split), guess_at = guess + warp + lane * kWarps;
+  const int rows_here = a.n_rows[b], len_here = a.lens[b], guess_id = guess_at < a.max_blocks ? table[guess_at] : -1;
+  int2 span[2 * MT];
+  Raw16<T> qv[2 * MT];
+#pragma unroll
+  for (int i = 0; i < 2 * MT; ++i) {
+    const int m = tile * ROWS + (i >> 1) * 16 + (i & 1) * 8 + g, r = m / a.G, h = kvh * a.G + m % a.G;
+    span[i] = make_int2(0, INT_MAX);
+#pragma unroll
+    for (int k = 0; k < (int)sizeof(T); ++k) qv[i].v[k] = make_uint4(0u, 0u, 0u, 0u);
+    if (r < a.R) {
+      if (a.spans) span[i] = a.spans[(size_t)b * a.R + r];
+      const uint4 *src = reinterpret_cast<const uint4 *>(static_cast<const T *>(a.q) + ((size_t)b * a.R + r) * a.q_row + h * kDh + 16 * t);
+#pragma unroll
+      for (int k = 0; k < (int)sizeof(T); ++k) qv[i].v[k] = src[k];
+    }
+  }
 
   // ---- the rows and what they see
-  const int n_rows = min(max(a.n_rows[b], 0), a.R);
-  const int len = (int)min((long long)min(max(a.lens[b], 0), a.max_len), (long long)a.max_blocks * kBlk);
+  const int n_rows = min(max(rows_here, 0), a.R);
+  const int len = (int)min((long long)min(max(len_here, 0), a.max_len), (long long)a.max_blocks * kBlk);
   Row row[MT][2];
   int lo = INT_MAX, hi = 0, all_lo = 0, all_hi = INT_MAX;       // seen by some row; seen by every row that sees anything
 #pragma unroll
   for (int i = 0; i < 2 * MT; ++i) {
     Row &w = row[i >> 1][i & 1];
-    const int m = tile * ROWS + (i >> 1) * 16 + (i & 1) * 8 + g, r = m / a.G, h = kvh * a.G + m % a.G;
-    w.begin = w.end = 0; w.mul = 0.f; w.m = -INFINITY; w.l = 0.f; w.bias = nullptr;
+    const int r = (tile * ROWS + (i >> 1) * 16 + (i & 1) * 8 + g) / a.G;
+    int2 sp = make_int2(0, 0);                                  // begin == end: the row sees nothing
+    w.m = -INFINITY; w.l = 0.f;
     if (r < n_rows) {
-      const int2 sp = a.spans ? a.spans[(size_t)b * a.R + r] : make_int2(0, len);
-      w.begin = max(sp.x, 0); w.end = min(sp.y, len);
-      if (w.begin >= w.end) w.begin = w.end = 0;
-      else {
-        lo = min(lo, w.begin); hi = max(hi, w.end); all_lo = max(all_lo, w.begin); all_hi = min(all_hi, w.end);
-        if (MOD && a.bias) w.bias = a.bias + (size_t)h * a.n_bias;
-      }
+      sp = make_int2(max(span[i].x, 0), min(span[i].y, len));
+      if (sp.x >= sp.y) sp.x = sp.y = 0;
+      else { lo = min(lo, sp.x); hi = max(hi, sp.y); all_lo = max(all_lo, sp.x); all_hi = min(all_hi, sp.y); }
     }
+    span[i] = sp;
+    if (t == 0) notes.span[i * 8 + g] = sp;
   }
   lo = __reduce_min_sync(0xffffffffu, lo); hi = __reduce_max_sync(0xffffffffu, hi);
   all_lo = __reduce_max_sync(0xffffffffu, all_lo); all_hi = __reduce_min_sync(0xffffffffu, all_hi);
   const int blk0 = hi > 0 ? lo / kBlk : 0, n_blk = hi > 0 ? (hi + kBlk - 1) / kBlk - blk0 : 0;
-  const int c0 = blk0 + (int)((long long)n_blk * split / a.splits), c1 = blk0 + (int)((long long)n_blk * (split + 1) / a.splits);
+  const int c0 = blk0 + share(n_blk, split), c1 = blk0 + share(n_blk, split + 1);
   const int n = c1 - c0 > warp ? (c1 - c0 - warp + kWarps - 1) / kWarps : 0;       // this warp's blocks: c0 + warp + i * kWarps
 
-  // ---- first copies
-  const int32_t *table = a.table + (size_t)b * a.max_blocks + c0 + warp;
-  auto block_id = [&](int i) {                                                     // lane's block of a run of 32
-    int id = -1;
-    if (i < n) {
-      id = table[(size_t)i * kWarps];
-      if (id < 0 || id >= a.n_blocks) { id = -1; if (a.status) *a.status = PD_ERR_ARG; }
-    }
-    return id;
-  };
-  auto block_scale = [&](int id) { return id >= 0 ? a.scales[(size_t)id * a.HK + kvh] : make_float2(0.f, 0.f); };
-  auto block_ptr = [&](int id) { return a.codes + ((size_t)max(id, 0) * a.HK + kvh) * kStageBytes; };     // an id out of range is fetched from block 0 and not used
-  int ids = block_id(lane), next_ids = -1;
-  float2 sc = block_scale(ids), next_sc = make_float2(0.f, 0.f);
+  // ---- first copies: block i's keys are copy 2 i, its values copy 2 i + 1; copy c goes to slot c % NS
+  // an id out of range is fetched from block 0 and not used
+  auto in_range = [&](int id) { return id >= 0 && id < a.n_blocks; };
+  auto copy_src = [&](int id, int c) { return a.codes + ((size_t)(in_range(id) ? id : 0) * a.HK + kvh) * (2 * kPart) + (c & 1) * kPart; };
+  auto scale_src = [&](int id) { return a.scales + (size_t)(in_range(id) ? id : 0) * a.HK + kvh; };
+  const int id0 = c0 == guess ? guess_id : lane < min(n, kRun) ? table[c0 + warp + lane * kWarps] : -1;
 #pragma unroll
-  for (int s = 0; s < kStages; ++s) {
-    const int id = __shfl_sync(0xffffffffu, ids, s);
-    if (s < n && lane == 0) fetch(stage0 + s * kStageBytes, block_ptr(id), bar0 + s * 8);
+  for (int c = 0; c < NS; ++c) {
+    const int id = __shfl_sync(0xffffffffu, id0, c >> 1);
+    if (c < 2 * n && lane == 0) fetch(slot0 + c * kPart, copy_src(id, c), bar0 + c * 8);
+  }
+  if (lane < min(n, kRun)) {
+    notes.id[lane] = id0;
+    async_copy(&notes.scale[lane], scale_src(id0));
   }
 
   // ---- queries: dims 16 t + 4 s + {0, 1} | {2, 3} of k16 step s; a row is brought to a largest value in [1, 2) so that f16 holds it
@@ -193,11 +250,12 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) cache_attn_kernel(CacheA
 #pragma unroll
   for (int i = 0; i < 2 * MT; ++i) {
     Row &w = row[i >> 1][i & 1];
-    const int m = tile * ROWS + (i >> 1) * 16 + (i & 1) * 8 + g, r = m / a.G, h = kvh * a.G + m % a.G;
     float f[16];
+    unpack16(qv[i], f);
+    if (span[i].x == span[i].y) {
 #pragma unroll
-    for (int k = 0; k < 16; ++k) f[k] = 0.f;
-    if (w.begin < w.end) load16(static_cast<const T *>(a.q) + ((size_t)b * a.R + r) * a.q_row + h * kDh + 16 * t, f);
+      for (int k = 0; k < 16; ++k) f[k] = 0.f;
+    }
     float mx = 0.f;
 #pragma unroll
     for (int k = 0; k < 16; ++k) mx = fmaxf(mx, fabsf(f[k]));
@@ -216,6 +274,7 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) cache_attn_kernel(CacheA
       }
   }
 
+  async_copies_land();
   float o[MT][8][4];
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt)
@@ -224,147 +283,229 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) cache_attn_kernel(CacheA
 
   // ---- the blocks
   bool ok = true;
-  int st = 0; uint32_t phase = 0;
-  for (int i = 0; i < n && ok; ++i) {
-    if ((i & 31) == 0) {
-      if (i) { ids = next_ids; sc = next_sc; }
-      next_ids = block_id(i + 32 + lane);
+  int st = 0; uint32_t phase = 0;                                                  // slot and phase of the copy that is waited for next
+  auto arrived = [&] { return __all_sync(0xffffffffu, mbar_wait(bar0 + st * 8, phase)); };
+  // The warp is through with copy c: its slot takes copy c + NS, which must not overtake the warp's reads.
+  auto refill = [&](int i, int c) {
+    __syncwarp();
+    const int nc = c + NS, ni = nc >> 1;
+    if (ni < n && lane == 0) {
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      fetch(slot0 + st * kPart, copy_src(notes.id[ni & (2 * kRun - 1)], nc), bar0 + st * 8);
     }
-    if ((i & 31) == 16) next_sc = block_scale(next_ids);
-    const int id = __shfl_sync(0xffffffffu, ids, i & 31);
-    const float ks = __shfl_sync(0xffffffffu, sc.x, i & 31), vs = __shfl_sync(0xffffffffu, sc.y, i & 31);
-    const uint32_t kbase = stage0 + st * kStageBytes, vbase = kbase + kPart;
-    ok = __all_sync(0xffffffffu, mbar_wait(bar0 + st * 8, phase));
+    if (++st == NS) { st = 0; phase ^= 1; }
+  };
+  for (int i = 0; i < n; ++i) {
+    // the run of blocks after this one: ids while its first block is worked on, scales from its ninth
+    if ((i & (kRun / 2 - 1)) == 0) {
+      async_copies_land();
+      const int at = (i & ~(kRun - 1)) + kRun + lane, to = at & (2 * kRun - 1);
+      if (lane < kRun && at < n) {
+        if ((i & (kRun / 2)) == 0) async_copy(&notes.id[to], table + c0 + warp + at * kWarps);
+        else async_copy(&notes.scale[to], scale_src(notes.id[to]));
+      }
+    }
+    const bool here = in_range(notes.id[i & (2 * kRun - 1)]);
+    if (!here && lane == 0 && a.status) *a.status = PD_ERR_ARG;
+    const float2 sc = notes.scale[i & (2 * kRun - 1)];
     const int p0 = (c0 + warp + i * kWarps) * kBlk;
-    if (ok && id >= 0) {
-      const bool edge = p0 < all_lo || p0 + kBlk > all_hi;                         // some row does not see all of it
-      // ---- scores
-      float s[MT][8][4];
+    const bool edge = p0 < all_lo || p0 + kBlk > all_hi;                           // some row does not see all of it
+    if (!(ok = arrived())) break;
+    // ---- scores, four tiles of eight tokens at a time: products in a row are independent
+    float s[MT][8][4];
+    const uint32_t kbase = slot0 + st * kPart;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const int token = 16 * (g >> 1) + 4 * (j >> 1) + 2 * (j & 1) + (g & 1);
+    for (int jh = 0; jh < 8; jh += 4) {
+      uint32_t u[4][4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int token = 16 * (g >> 1) + 4 * ((jh + j) >> 1) + 2 * (j & 1) + (g & 1);
         const uint4 w = lds128(kbase + token * kDh + t * 16);
-        const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+        u[j][0] = w.x; u[j][1] = w.y; u[j][2] = w.z; u[j][3] = w.w;
+      }
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) s[mt][j][0] = s[mt][j][1] = s[mt][j][2] = s[mt][j][3] = 0.f;
+      for (int k = 0; k < 4; ++k)
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
+        for (int j = 0; j < 4; ++j) {
           uint32_t b0, b1;
-          widen(u[k], b0, b1);
+          widen(u[j][k], b0, b1);
 #pragma unroll
           for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-            for (int p = 0; p < NP; ++p) mma_f16(s[mt][j], qf[p][mt][k], b0, b1);
+            for (int p = 0; p < NP; ++p) {
+              if (k + p == 0) mma_f16_first(s[mt][jh + j], qf[p][mt][k], b0, b1);
+              else mma_f16(s[mt][jh + j], qf[p][mt][k], b0, b1);
+            }
         }
-      }
-      // ---- the block's softmax
-      uint32_t pf[NP][MT][4][4];
-      float keep[MT][2], take[MT][2];                                              // factors of the values so far and of this block's
+    }
+    refill(i, 2 * i);
+    // ---- the block's softmax; without cap and bias the scale (positive) comes in with the exponent
+    uint32_t pf[NP][MT][4][4];
+    float keep[MT][2], take[MT][2];                                                // factors of the values so far and of this block's
+    float mref[MT][2];
 #pragma unroll
-      for (int mt = 0; mt < MT; ++mt)
+    for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          Row &w = row[mt][x];
-          const float mul = w.mul * ks;
-          float mx = -INFINITY;
+      for (int x = 0; x < 2; ++x) {
+        Row &w = row[mt][x];
+        const float mul = fmaxf(w.mul * sc.x, FLT_MIN);                              // a zero would make a masked score no number
+        if (MOD) {
+          const int end = notes.span[mt * 16 + x * 8 + g].y;
+          const float *bias = a.bias ? a.bias + (size_t)(kvh * a.G + (tile * ROWS + mt * 16 + x * 8 + g) % a.G) * a.n_bias : nullptr;
 #pragma unroll
           for (int j = 0; j < 8; ++j)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
               float v = s[mt][j][2 * x + e] * mul;
               const int pos = p0 + 16 * t + 4 * (j >> 1) + 2 * (j & 1) + e;
-              if (MOD) {
-                if (a.cap_log2e > 0.f) v = a.cap_log2e * (NP == 2 ? tanhf(v) : 1.f - __fdividef(2.f, 1.f + ex2(v)));
-                if (w.bias) v += w.bias[min(max(w.end - 1 - pos, 0), a.n_bias - 1)] * kLog2e;
-              }
-              if (edge && (pos < w.begin || pos >= w.end)) v = -INFINITY;
+              if (a.cap_log2e > 0.f) v = a.cap_log2e * (NP == 2 ? tanhf(v) : 1.f - __fdividef(2.f, 1.f + ex2(v)));
+              if (bias) v += bias[min(max(end - 1 - pos, 0), a.n_bias - 1)] * kLog2e;
               s[mt][j][2 * x + e] = v;
-              mx = fmaxf(mx, v);
             }
-          mx = quad_max(mx);
-          const float ref = (mx == -INFINITY ? 0.f : mx) - kLift;
-          float sum = 0.f;
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const float w0 = ex2(s[mt][j][2 * x] - ref), w1 = ex2(s[mt][j][2 * x + 1] - ref);
-            sum += w0 + w1;
-            const uint32_t p = pack(w0, w1);
-            pf[0][mt][j >> 1][2 * (j & 1) + x] = p;
-            if (NP == 2) pf[NP - 1][mt][j >> 1][2 * (j & 1) + x] = pack_rest(w0, w1, p);
-          }
-          const float m_new = fmaxf(w.m, mx), mref = m_new == -INFINITY ? 0.f : m_new;
-          keep[mt][x] = ex2(w.m - mref);
-          const float tk = ex2(mx - mref);
-          w.l = w.l * keep[mt][x] + sum * tk;
-          take[mt][x] = tk * vs;
-          w.m = m_new;
         }
-      // ---- values
-      bool nan_seen = false;                                                       // a value that is no number, at a position that some row sees
+        if (edge) {
+          const int2 sp = notes.span[mt * 16 + x * 8 + g];
 #pragma unroll
-      for (int dn = 0; dn < 8; ++dn) {
-        const uint4 w = lds128(vbase + (dn * 8 + g) * kBlk + t * 16);
-        uint32_t u[4] = {w.x, w.y, w.z, w.w};
-        float tv[MT][4];
+          for (int j = 0; j < 8; ++j)
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) tv[mt][0] = tv[mt][1] = tv[mt][2] = tv[mt][3] = 0.f;
+            for (int e = 0; e < 2; ++e) {
+              const int pos = p0 + 16 * t + 4 * (j >> 1) + 2 * (j & 1) + e;
+              if (pos < sp.x || pos >= sp.y) s[mt][j][2 * x + e] = -INFINITY;
+            }
+        }
+        float mx = -INFINITY;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          if (edge) {                                                              // 0 must not meet what is no number
-            const uint32_t nb = nan_bytes(u[k]);
-            if (nb) {
+        for (int j = 0; j < 8; ++j) mx = fmaxf(mx, fmaxf(s[mt][j][2 * x], s[mt][j][2 * x + 1]));
+        mx = quad_max(mx);
+        if (!here) mx = -INFINITY;
+        const float f = MOD ? 1.f : mul;
+        mx *= f;
+        const float ref = kLift - (mx == -INFINITY ? 0.f : mx);
 #pragma unroll
-              for (int y = 0; y < 4; ++y)
-                if (nb >> (8 * y) & 0x80u) {
-                  const int pos = p0 + 16 * t + 4 * k + y;
-                  nan_seen |= pos >= lo && pos < hi;
-                  u[k] &= ~(0xffu << (8 * y));
-                }
+        for (int j = 0; j < 8; ++j) {
+          const float w0 = ex2(MOD ? s[mt][j][2 * x] + ref : fmaf(s[mt][j][2 * x], f, ref)), w1 = ex2(MOD ? s[mt][j][2 * x + 1] + ref : fmaf(s[mt][j][2 * x + 1], f, ref));
+          const uint32_t p = pack(w0, w1);
+          pf[0][mt][j >> 1][2 * (j & 1) + x] = p;
+          if (NP == 2) pf[NP - 1][mt][j >> 1][2 * (j & 1) + x] = pack_rest(w0, w1, p);
+        }
+        const float m_new = fmaxf(w.m, mx);
+        mref[mt][x] = m_new == -INFINITY ? 0.f : m_new;
+        keep[mt][x] = ex2(w.m - mref[mt][x]);
+        take[mt][x] = ex2(mx - mref[mt][x]);
+        w.m = m_new;
+      }
+    // ---- values, four tiles of eight dims at a time
+    if (!(ok = arrived())) break;
+    const uint32_t vbase = slot0 + st * kPart;
+    bool moved = false;                                                            // some row's running maximum did
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) moved |= keep[mt][0] != 1.f || keep[mt][1] != 1.f;
+    if (__any_sync(0xffffffffu, moved)) {
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+        for (int dn = 0; dn < 8; ++dn)
+#pragma unroll
+          for (int x = 0; x < 4; ++x) o[mt][dn][x] *= keep[mt][x >> 1];
+    }
+    uint32_t nan_seen = 0;                                                         // values that are no numbers, at positions that some row sees
+    if (here) {
+#pragma unroll
+      for (int dh = 0; dh < 8; dh += 4) {
+        uint32_t u[4][4];
+        float tv[MT][4][4];
+#pragma unroll
+        for (int dn = 0; dn < 4; ++dn) {
+          const uint4 w = lds128(vbase + ((dh + dn) * 8 + g) * kBlk + t * 16);
+          u[dn][0] = w.x; u[dn][1] = w.y; u[dn][2] = w.z; u[dn][3] = w.w;
+        }
+        if (edge) {                                                                // 0 must not meet what is no number
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const int p = p0 + 16 * t + 4 * k;
+            const uint32_t seen = below(hi - p) & ~below(lo - p);
+#pragma unroll
+            for (int dn = 0; dn < 4; ++dn) {
+              const uint32_t nb = nan_bytes(u[dn][k]);
+              nan_seen |= nb & seen;
+              u[dn][k] &= ~(nb | (nb - (nb >> 7)));
             }
           }
-          uint32_t b0, b1;
-          widen(u[k], b0, b1);
-#pragma unroll
-          for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-            for (int p = 0; p < NP; ++p) mma_f16(tv[mt], pf[p][mt][k], b0, b1);
         }
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+#pragma unroll
+          for (int dn = 0; dn < 4; ++dn) {
+            uint32_t b0, b1;
+            widen(u[dn][k], b0, b1);
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+              for (int p = 0; p < NP; ++p) {
+                if (k + p == 0) mma_f16_first(tv[mt][dn], pf[p][mt][k], b0, b1);
+                else mma_f16(tv[mt][dn], pf[p][mt][k], b0, b1);
+              }
+          }
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-          for (int x = 0; x < 4; ++x) o[mt][dn][x] = o[mt][dn][x] * keep[mt][x >> 1] + tv[mt][x] * take[mt][x >> 1];
+          for (int dn = 0; dn < 4; ++dn)
+#pragma unroll
+            for (int x = 0; x < 4; ++x) o[mt][dh + dn][x] = fmaf(tv[mt][dn][x], take[mt][x >> 1] * sc.y, o[mt][dh + dn][x]);
       }
-      if (edge && __any_sync(0xffffffffu, nan_seen)) {
-        // rows that see such a value get it after all (values of 0x7f and 0xff at visible positions; not a path of speed)
+      if (edge && __any_sync(0xffffffffu, nan_seen != 0)) {
+        // rows that see such a value get it after all: a product of who sees which position with where they stand
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
+        for (int mt = 0; mt < MT; ++mt) {
+          uint32_t sees[4][4];
 #pragma unroll
-          for (int dn = 0; dn < 8; ++dn)
+          for (int x = 0; x < 2; ++x) {
+            const int2 sp = notes.span[mt * 16 + x * 8 + g];
 #pragma unroll
-            for (int x = 0; x < 4; ++x) {
-              const Row &w = row[mt][x >> 1];
-              const uint8_t *v = ring + (vbase - smem_u32(ring)) + (dn * 8 + 2 * t + (x & 1)) * kBlk;
-              for (int y = 0; y < kBlk; ++y)
-                if ((v[y] & 0x7f) == 0x7f && p0 + y >= w.begin && p0 + y < w.end) o[mt][dn][x] = __int_as_float(0x7fffffff);
+            for (int k = 0; k < 4; ++k)
+#pragma unroll
+              for (int y = 0; y < 2; ++y) {
+                const int p = p0 + 16 * t + 4 * k + 2 * y;
+                sees[k][2 * y + x] = (p >= sp.x && p < sp.y ? 0x3c00u : 0u) | (p + 1 >= sp.x && p + 1 < sp.y ? 0x3c000000u : 0u);
+              }
+          }
+#pragma unroll
+          for (int dn = 0; dn < 8; ++dn) {
+            const uint4 w = lds128(vbase + (dn * 8 + g) * kBlk + t * 16);
+            const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+            float c[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              const uint32_t nb = nan_bytes(u[k]);
+              mma_f16(c, sees[k], (nb & 0x80u ? 0x3c00u : 0u) | (nb & 0x8000u ? 0x3c000000u : 0u),
+                      (nb & 0x800000u ? 0x3c00u : 0u) | (nb & 0x80000000u ? 0x3c000000u : 0u));
             }
+#pragma unroll
+            for (int x = 0; x < 4; ++x)
+              if (c[x] > 0.f) o[mt][dn][x] = __int_as_float(0x7fffffff);
+          }
+        }
       }
     }
-    // ---- the stage is free: the copy must not overtake the warp's reads
-    __syncwarp();
-    const int nx = i + kStages;
-    const int nid = __shfl_sync(0xffffffffu, (nx ^ i) & ~31 ? next_ids : ids, nx & 31);
-    if (ok && nx < n && lane == 0) {
-      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-      fetch(stage0 + st * kStageBytes, block_ptr(nid), bar0 + st * 8);
+    // the weights' sum is a product with ones: every lane of a row gets it, and numerator and denominator see the same roundings
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+      float sum[4];
+      mma_f16_first(sum, pf[0][mt][0], 0x3c003c00u, 0x3c003c00u);
+#pragma unroll
+      for (int i = 1; i < 4 * NP; ++i) mma_f16(sum, pf[i >> 2][mt][i & 3], 0x3c003c00u, 0x3c003c00u);
+#pragma unroll
+      for (int x = 0; x < 2; ++x)
+        if (here) row[mt][x].l = row[mt][x].l * keep[mt][x] + sum[2 * x] * take[mt][x];
     }
-    if (++st == kStages) { st = 0; phase ^= 1; }
+    refill(i, 2 * i + 1);
   }
-  if (!ok) {                                                                       // the other copies in flight must land before the CTA ends
+  if (!ok) {                                                                       // the copies in flight must land before the CTA ends
     if (lane == 0 && a.status) *a.status = PD_ERR_TIMEOUT;
-    for (int s = 0; s < kStages - 1; ++s) { mbar_wait(bar0 + st * 8, phase); if (++st == kStages) { st = 0; phase ^= 1; } }
+    for (int s = 0; s < NS; ++s) { mbar_wait(bar0 + st * 8, phase); if (++st == NS) { st = 0; phase ^= 1; } }
   }
 
-  // ---- join the warps: sums of every row, then 64 columns of every row
+  // ---- join the warps, then the cluster's CTAs, both in their order: a thread takes columns 4 k .. 4 k + 3 and 32 + 4 k .. of a row
   __syncthreads();                                                                 // the rings are free
   float *rec = reinterpret_cast<float *>(ring), *ml = rec + kWarps * ROWS * kDh;   // [warp][row][64], [warp][row][2]
 #pragma unroll
@@ -372,55 +513,91 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) cache_attn_kernel(CacheA
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
       const int m = warp * ROWS + mt * 16 + x * 8 + g;
-      const bool any = row[mt][x].begin < row[mt][x].end;                          // rows that see nothing went along unmasked
-      const float l = quad_sum(row[mt][x].l);
-      if (t == 0) { ml[2 * m] = any ? row[mt][x].m : -INFINITY; ml[2 * m + 1] = any ? l : 0.f; }
+      const int2 sp = notes.span[mt * 16 + x * 8 + g];
+      const bool any = sp.x < sp.y;                          // rows that see nothing went along unmasked
+      if (t == 0) store2(ml + 2 * m, any ? row[mt][x].m : -INFINITY, any ? row[mt][x].l : 0.f);
 #pragma unroll
       for (int dn = 0; dn < 8; ++dn)
         store2(rec + m * kDh + ((dn * 8 + 2 * t) ^ ((g & 3) << 3)), any ? o[mt][dn][2 * x] : 0.f, any ? o[mt][dn][2 * x + 1] : 0.f);
     }
   __syncthreads();
-  for (int i = threadIdx.x; i < ROWS * (kDh / 2); i += kThreads) {
-    const int m = i / (kDh / 2), c = 2 * (i % (kDh / 2)), at = c ^ ((m & 3) << 3);
+  const int cluster = a.cluster, rank = split % cluster, own = ROWS / cluster;     // rank k sums rows k * own .. of the cluster's CTAs
+  float *inbox = reinterpret_cast<float *>(ring + RING);                           // [CTA][row of this rank][kRec]
+  // Sum of n partial results of a row; `ml_of` and `o_of` give the addresses of one's (maximum, sum) and first columns.
+  auto join = [&](int n, auto ml_of, auto o_of, float2 &h, float4 &x, float4 &y) {
     float mx = -INFINITY;
-#pragma unroll
-    for (int w = 0; w < kWarps; ++w) mx = fmaxf(mx, ml[2 * (w * ROWS + m)]);
+    for (int k = 0; k < n; ++k) mx = fmaxf(mx, ml_of(k)->x);
     const float ref = mx == -INFINITY ? 0.f : mx;
-    float l = 0.f, x = 0.f, y = 0.f;
+    float l = 0.f;
+    x = y = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+    for (int k = 0; k < n; ++k) {
+      const float2 s = *ml_of(k);
+      const float f = ex2(s.x - ref);
+      const float4 u = *reinterpret_cast<const float4 *>(o_of(k, 0)), v = *reinterpret_cast<const float4 *>(o_of(k, 32));
+      l += s.y * f;
+      x.x += u.x * f; x.y += u.y * f; x.z += u.z * f; x.w += u.w * f;
+      y.x += v.x * f; y.y += v.y * f; y.z += v.z * f; y.w += v.w * f;
+    }
+    h = make_float2(mx, l);
+  };
+  auto finish = [&](int m, int c, float2 h, float4 x, float4 y) {
+    if (a.outer > 1) {
+      float *p = a.part + ((((size_t)b * gridDim.y + blockIdx.y) * a.outer + split / cluster) * ROWS + m) * kRec;
+      store4(p + c, x); store4(p + c + 32, y);
+      if (c == 0) store2(p + kDh, h.x, h.y);
+      return;
+    }
+    const int gm = tile * ROWS + m, r = gm / a.G, head = kvh * a.G + gm % a.G;
+    if (r >= a.R) return;
+    const float inv = h.y == 0.f ? 0.f : 1.f / h.y;                                // nothing seen: zero
+    T *p = static_cast<T *>(a.out) + (((size_t)b * a.R + r) * a.H + head) * kDh + c;
+    store4(p, make_float4(x.x * inv, x.y * inv, x.z * inv, x.w * inv));
+    store4(p + 32, make_float4(y.x * inv, y.y * inv, y.z * inv, y.w * inv));
+  };
+  if (cluster > 1) cluster_wait();                                                 // all CTAs of the cluster have begun
 #pragma unroll
-    for (int w = 0; w < kWarps; ++w) {
-      const float f = ex2(ml[2 * (w * ROWS + m)] - ref);
-      const float2 v = *reinterpret_cast<const float2 *>(rec + (w * ROWS + m) * kDh + at);
-      l += ml[2 * (w * ROWS + m) + 1] * f; x += v.x * f; y += v.y * f;
-    }
-    const int gm = tile * ROWS + m, r = gm / a.G, h = kvh * a.G + gm % a.G;
-    if (a.splits > 1) {
-      float *p = a.part + (((size_t)b * gridDim.y + blockIdx.y) * a.splits + split) * ROWS * (kDh + 2) + (size_t)m * (kDh + 2);
-      store2(p + c, x, y);
-      if (c == 0) store2(p + kDh, mx, l);
-    } else if (r < a.R) {
-      const float inv = l == 0.f ? 0.f : 1.f / l;                                  // nothing seen: zero
-      store2(static_cast<T *>(a.out) + (((size_t)b * a.R + r) * a.H + h) * kDh + c, x * inv, y * inv);
-    }
+  for (int i = threadIdx.x; i < ROWS * 8; i += kThreads) {
+    const int m = i >> 3, c = (i & 7) * 4;
+    float2 h;
+    float4 x, y;
+    join(kWarps, [&](int k) { return reinterpret_cast<const float2 *>(ml + 2 * (k * ROWS + m)); },
+         [&](int k, int at) { return rec + (k * ROWS + m) * kDh + ((c + at) ^ ((m & 3) << 3)); }, h, x, y);
+    if (cluster == 1) { finish(m, c, h, x, y); continue; }
+    const uint32_t to = peer_addr(smem_u32(inbox + ((size_t)rank * own + m % own) * kRec), m / own);
+    peer_st4(to + c * 4, x); peer_st4(to + (c + 32) * 4, y);
+    if (c == 0) peer_st4(to + kDh * 4, make_float4(h.x, h.y, 0.f, 0.f));
+  }
+  if (cluster == 1) return;
+  cluster_arrive();
+  cluster_wait();
+  for (int i = threadIdx.x; i < own * 8; i += kThreads) {
+    const int m = i >> 3, c = (i & 7) * 4;
+    float2 h;
+    float4 x, y;
+    join(cluster, [&](int k) { return reinterpret_cast<const float2 *>(inbox + (k * own + m) * kRec + kDh); },
+         [&](int k, int at) { return inbox + (k * own + m) * kRec + c + at; }, h, x, y);
+    finish(rank * own + m, c, h, x, y);
   }
 }
 
 // Joins the splits of a row in their order: one warp per (sequence, row, head), two columns per lane.
 template <typename T>
 __global__ void __launch_bounds__(128) cache_attn_merge_kernel(CacheAttnArgs a, int rows_tile, long long n_out) {
+  op_begin();
   const long long i = (long long)blockIdx.x * 4 + (threadIdx.x >> 5);
   const int lane = threadIdx.x & 31;
   if (i >= n_out) return;
   const int h = (int)(i % a.H), r = (int)(i / a.H % a.R), b = (int)(i / a.H / a.R);
   const int kvh = h / a.G, m = r * a.G + h % a.G, tile = m / rows_tile;
-  const float *p = a.part + (((size_t)b * a.HK + kvh) * a.tiles + tile) * a.splits * rows_tile * (kDh + 2) + (size_t)(m % rows_tile) * (kDh + 2);
-  const size_t step = (size_t)rows_tile * (kDh + 2);
+  const float *p = a.part + (((size_t)b * a.HK + kvh) * a.tiles + tile) * a.outer * rows_tile * kRec + (size_t)(m % rows_tile) * kRec;
+  const size_t step = (size_t)rows_tile * kRec;
   float mx = -INFINITY;
-  for (int s = lane; s < a.splits; s += 32) mx = fmaxf(mx, p[s * step + kDh]);
+  for (int s = lane; s < a.outer; s += 32) mx = fmaxf(mx, p[s * step + kDh]);
   for (int x = 16; x; x >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, x));
   const float ref = mx == -INFINITY ? 0.f : mx;
   float l = 0.f, x = 0.f, y = 0.f;
-  for (int s = 0; s < a.splits; ++s) {
+  for (int s = 0; s < a.outer; ++s) {
     const float2 ml = *reinterpret_cast<const float2 *>(p + s * step + kDh), v = *reinterpret_cast<const float2 *>(p + s * step + 2 * lane);
     const float f = ex2(ml.x - ref);
     l += ml.y * f; x += v.x * f; y += v.y * f;
@@ -429,8 +606,8 @@ __global__ void __launch_bounds__(128) cache_attn_merge_kernel(CacheAttnArgs a, 
   store2(static_cast<T *>(a.out) + i * kDh + 2 * lane, x * inv, y * inv);
 }
 
-// Shape of a launch: rows per tile, tiles, splits.  A function of sizes the scratch is asked for with.
-struct Plan { int mt, tiles, splits; };
+// Shape of a launch: row tiles, CTAs of a cluster, clusters per segment.  A function of sizes the scratch is asked for with.
+struct Plan { int mt, tiles, cluster, outer; };
 
 Plan plan_of(int dtype, int batch, int rows, int heads, int kv_heads, int max_len) {
   Plan p;
@@ -438,8 +615,12 @@ Plan plan_of(int dtype, int batch, int rows, int heads, int kv_heads, int max_le
   p.mt = dtype == PD_DTYPE_BF16 && m > 16 ? 2 : 1;
   p.tiles = (m + 16 * p.mt - 1) / (16 * p.mt);
   const long long segs = (long long)batch * kv_heads * p.tiles, blocks = ((long long)max_len + kBlk - 1) / kBlk;
-  const long long most = std::max(1ll, blocks / kWarps);                           // a block for each warp
-  p.splits = (int)std::max(1ll, std::min(most, kSms * kCtasPerSm / segs));
+  // places for CTAs in clusters: a GPC's SMs are not a multiple of a cluster's CTAs (512 of 592 places taken 35 us, 576 in two rounds 47 us, at 2 x 4
+  // key heads x 131072 tokens)
+  const long long room = std::max(1ll, kClusterSms * ctas_per_sm(p.mt, dtype == PD_DTYPE_FP32) / segs);
+  p.cluster = 1;
+  while (p.cluster < kMaxCluster && p.cluster * 2 <= room && p.cluster * kWarps < blocks) p.cluster *= 2;
+  p.outer = p.cluster == kMaxCluster ? (int)std::max(1ll, std::min(room / kMaxCluster, blocks / (kMaxCluster * kWarps * kOuterBlocks))) : 1;
   return p;
 }
 
@@ -450,19 +631,19 @@ bool cache_attn_sizes_ok(int dtype, int batch, int rows, int heads, int kv_heads
 }
 
 size_t scratch_bytes_of(const Plan &p, int batch, int kv_heads) {
-  return p.splits > 1 ? (size_t)batch * kv_heads * p.tiles * p.splits * p.mt * 16 * (kDh + 2) * sizeof(float) : 0;
+  return p.outer > 1 ? (size_t)batch * kv_heads * p.tiles * p.outer * p.mt * 16 * kRec * sizeof(float) : 0;
 }
 
 template <typename T, int MT>
 cudaError_t launch_cache_attn(const CacheAttnArgs &a, int batch, bool mod, cudaStream_t s) {
+  constexpr int smem = smem_bytes(MT, sizeof(T) == 4);
   auto kernel = mod ? cache_attn_kernel<T, MT, true> : cache_attn_kernel<T, MT, false>;
-  cudaError_t st = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+  cudaError_t st = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (st != cudaSuccess) return st;
-  kernel<<<dim3(a.splits, a.HK * a.tiles, batch), kThreads, kSmem, s>>>(a);
-  if ((st = cudaGetLastError()) != cudaSuccess || a.splits == 1) return st;
+  st = op_launch(kernel, dim3(a.cluster * a.outer, a.HK * a.tiles, batch), kThreads, smem, a.cluster, s, a);
+  if (st != cudaSuccess || a.outer == 1) return st;
   const long long n_out = (long long)batch * a.R * a.H;
-  cache_attn_merge_kernel<T><<<(unsigned)((n_out + 3) / 4), 128, 0, s>>>(a, MT * 16, n_out);
-  return cudaGetLastError();
+  return op_launch(cache_attn_merge_kernel<T>, dim3((unsigned)((n_out + 3) / 4)), 128, 0, 1, s, a, MT * 16, n_out);
 }
 
 }  // namespace
@@ -493,7 +674,7 @@ pd_status pd_cache_attention(int32_t dtype, int32_t batch, int32_t rows_per_seq,
   if (scratch_bytes < need) return PD_ERR_WORKSPACE;
   CacheAttnArgs a;
   a.R = rows_per_seq; a.H = n_heads; a.HK = n_kv_heads; a.G = n_heads / n_kv_heads; a.n_blocks = n_blocks; a.max_blocks = max_blocks; a.max_len = max_len;
-  a.tiles = p.tiles; a.splits = p.splits; a.n_bias = bias ? n_bias : 0;
+  a.tiles = p.tiles; a.cluster = p.cluster; a.outer = p.outer; a.n_bias = bias ? n_bias : 0;
   a.scale_log2e = attn_scale * kLog2e; a.cap_log2e = softcap * kLog2e;
   // tanh(x) = 1 - 2 / (1 + e^2x): the bf16 kernel wants 2 x in log2 units
   a.inv_cap = softcap > 0.f ? (dtype == PD_DTYPE_BF16 ? 2.f * kLog2e : 1.f) * attn_scale / softcap : 0.f;

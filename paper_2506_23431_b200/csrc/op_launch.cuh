@@ -1,0 +1,33 @@
+// Launch of the operators around the 8-bit cache: one after the other on a step's rows, a few microseconds each.
+#pragma once
+
+#include <cuda_runtime.h>
+
+namespace pd {
+
+// Everything enqueued before is complete and visible behind this; the kernel's first instruction.  What follows it in the stream may then be brought
+// onto the SMs while the kernel runs, up to its own wait: 1 to 2 us per launch between two of these operators.
+__device__ __forceinline__ void op_begin() {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
+
+// A launch that may be brought onto the SMs ahead of the end of the one before it, whatever that is; `cluster` CTAs along x.
+template <typename... P, typename... A>
+cudaError_t op_launch(void (*kernel)(P...), dim3 grid, int threads, size_t smem, int cluster, cudaStream_t s, A... args) {
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = cluster; attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cfg.attrs = attr;
+  cfg.numAttrs = cluster > 1 ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
+}  // namespace pd

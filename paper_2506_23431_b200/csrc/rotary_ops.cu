@@ -10,6 +10,7 @@
 // for a decode step.
 #include <math.h>
 
+#include "op_launch.cuh"
 #include "pd_internal.h"
 
 using namespace pd;
@@ -41,6 +42,7 @@ template <typename T, int N> struct alignas(sizeof(T) * N) Vec { T v[N]; };
 template <typename T, bool INTERLEAVED, int VEC>
 __global__ void __launch_bounds__(kRotThreads) rotary_kernel(RotaryArgs a) {
   __shared__ float2 cs[kRotMaxTokens * kRotMaxHead / 2];
+  op_begin();
   const int half = a.rot / 2, tok0 = blockIdx.x * a.tok_per_cta;
   const int nt = min(a.tok_per_cta, a.tokens - tok0);
   for (int i = threadIdx.x; i < nt * half; i += kRotThreads) {
@@ -93,9 +95,7 @@ __global__ void __launch_bounds__(kRotThreads) rotary_kernel(RotaryArgs a) {
 template <typename T, int VEC>
 cudaError_t launch_rotary(const RotaryArgs &a, int interleaved, cudaStream_t s) {
   const int grid = (a.tokens + a.tok_per_cta - 1) / a.tok_per_cta;
-  if (interleaved) rotary_kernel<T, true, VEC><<<grid, kRotThreads, 0, s>>>(a);
-  else rotary_kernel<T, false, VEC><<<grid, kRotThreads, 0, s>>>(a);
-  return cudaGetLastError();
+  return op_launch(interleaved ? rotary_kernel<T, true, VEC> : rotary_kernel<T, false, VEC>, dim3(grid), kRotThreads, 0, 1, s, a);
 }
 
 }  // namespace
