@@ -10,9 +10,11 @@
 // exact: the codes do not depend on the precision they are computed in, and a block whose scale grows keeps its older
 // codes bit for bit, but for those that leave the normal range.
 //
-// One CTA per (block, head): 128 threads take the keys, 128 the values.  A thread holds four tokens of eight dims, so that it
+// One CTA per (head, keys | values), walking a sequence's blocks.  A thread holds four tokens of eight dims, so that it
 // writes keys as 8 bytes per token and values, whose layout is turned, as whole words of four tokens, with no pass through shared memory.
 #include <cuda_fp16.h>
+
+#include <algorithm>
 
 #include "op_launch.cuh"
 #include "pd_internal.h"
@@ -23,6 +25,7 @@ namespace {
 
 constexpr int kBlk = PD_CACHE_BLOCK;
 constexpr int kPart = kBlk * kDh;                 // codes of a block's keys (values) of one head
+constexpr long long kAppendCtas = 24 * kSms;
 
 struct AppendArgs {
   int heads, n_blocks, max_blocks, rows, max_new;
@@ -55,13 +58,17 @@ __device__ __forceinline__ int scale_exponent(uint32_t amax_bits) {
 }
 __device__ __forceinline__ float pow2(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }      // -126 <= e <= 127
 
-__device__ __forceinline__ void load8(const float *p, float (&f)[8]) {
-  const float4 a = *reinterpret_cast<const float4 *>(p), b = *reinterpret_cast<const float4 *>(p + 4);
-  f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
+// Eight dims of a token as they lie in memory (zeros where there is no new token), and as numbers.
+template <typename T> struct Raw8 { uint4 v[sizeof(T) / 2]; };
+__device__ __forceinline__ void unpack8(const Raw8<float> &r, float (&f)[8]) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    f[4 * i] = __uint_as_float(r.v[i].x); f[4 * i + 1] = __uint_as_float(r.v[i].y);
+    f[4 * i + 2] = __uint_as_float(r.v[i].z); f[4 * i + 3] = __uint_as_float(r.v[i].w);
+  }
 }
-__device__ __forceinline__ void load8(const __nv_bfloat16 *p, float (&f)[8]) {
-  const uint4 w = *reinterpret_cast<const uint4 *>(p);
-  const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+__device__ __forceinline__ void unpack8(const Raw8<__nv_bfloat16> &r, float (&f)[8]) {
+  const uint32_t u[4] = {r.v[0].x, r.v[0].y, r.v[0].z, r.v[0].w};
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     f[2 * i] = __uint_as_float(u[i] << 16);
@@ -69,98 +76,145 @@ __device__ __forceinline__ void load8(const __nv_bfloat16 *p, float (&f)[8]) {
   }
 }
 
+// Largest magnitude so far, by its bits, NaN left out: two at a time in bf16.
+struct AbsMax32 {
+  float m = 0.f;
+  __device__ __forceinline__ void add(const Raw8<float> &r) {
+    float f[8];
+    unpack8(r, f);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = fmaxf(m, fabsf(f[i]));
+  }
+  __device__ __forceinline__ uint32_t bits() const { return __float_as_uint(m); }
+};
+struct AbsMax16 {
+  __nv_bfloat162 m = __floats2bfloat162_rn(0.f, 0.f);
+  __device__ __forceinline__ void add(const Raw8<__nv_bfloat16> &r) {
+    const uint32_t u[4] = {r.v[0].x, r.v[0].y, r.v[0].z, r.v[0].w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) m = __hmax2(m, __habs2(*reinterpret_cast<const __nv_bfloat162 *>(&u[i])));
+  }
+  __device__ __forceinline__ uint32_t bits() const {
+    const uint32_t w = *reinterpret_cast<const uint32_t *>(&m);
+    return max(w << 16, w & 0xffff0000u);
+  }
+};
+template <typename T> struct AbsMaxOf { using type = AbsMax32; };
+template <> struct AbsMaxOf<__nv_bfloat16> { using type = AbsMax16; };
+
 template <typename T>
-__global__ void __launch_bounds__(256) cache_append_kernel(AppendArgs a) {
+__global__ void __launch_bounds__(128, 8) cache_append_kernel(AppendArgs a) {
+  __shared__ uint32_t warp_max[2][4];
   op_begin();
-  const int b = blockIdx.z, h = blockIdx.y, is_v = threadIdx.x >> 7, t = threadIdx.x & 127;
-  const long long n = a.n_new[b], p0 = a.pos_start[b], row0 = a.row_start[b];
+  const int b = blockIdx.z, h = blockIdx.x >> 1, is_v = blockIdx.x & 1, warp = threadIdx.x >> 5, t = threadIdx.x;
+  const int n = a.n_new[b], p0 = a.pos_start[b], row0 = a.row_start[b];
   if (n <= 0) return;
-  const long long j = p0 / kBlk + blockIdx.x;                                     // block of the sequence
-  const int lo = (int)max(p0 - j * kBlk, 0ll), hi = (int)min(p0 + n - j * kBlk, (long long)kBlk);
-  if (p0 >= 0 && hi <= 0) return;                                                 // the sequence's tokens end before this block
-  const bool fits = n <= a.max_new && p0 >= 0 && row0 >= 0 && row0 + n <= a.rows && j < a.max_blocks;
-  const int id = fits ? a.table[(size_t)b * a.max_blocks + j] : -1;
-  if (id < 0 || id >= a.n_blocks) {
-    if (threadIdx.x == 0 && h == 0 && a.status) *a.status = PD_ERR_ARG;
+  if (n > a.max_new || p0 < 0 || row0 < 0 || (long long)row0 + n > a.rows) {
+    if (threadIdx.x == 0 && a.status) *a.status = PD_ERR_ARG;
     return;
   }
-  const size_t part = ((size_t)id * a.heads + h) * 2 + is_v;
   // four tokens of eight dims; keys: neighbouring lanes share a token, values: they share dims
   const int dg = is_v ? t >> 4 : t & 7, tg = is_v ? t & 15 : t >> 3;
-  const T *src = static_cast<const T *>(is_v ? a.v : a.k) + h * kDh + dg * 8;
-  const long long stride = is_v ? a.v_stride : a.k_stride, first = row0 + j * kBlk - p0 + tg * 4;
-  const float had = lo > 0 ? a.scales[part] : 0.f;
-  float f[4][8];
-  uint32_t amax = 0;
+  const long long stride = is_v ? a.v_stride : a.k_stride, end = (long long)p0 + n;
+  const T *src = static_cast<const T *>(is_v ? a.v : a.k) + h * kDh + dg * 8 + (row0 - (long long)p0 + tg * 4) * stride;     // the four tokens in block 0
+  const int32_t *table = a.table + (size_t)b * a.max_blocks;
+  const int j1 = (int)((end - 1) / kBlk);
+  int turn = 0;
+  for (int j = p0 / kBlk + blockIdx.y; j <= j1; j += gridDim.y, turn ^= 1) {      // blocks of the sequence
+    const int lo = max(p0 - j * kBlk, 0), hi = (int)min(end - (long long)j * kBlk, (long long)kBlk);
+    const int id = j < a.max_blocks ? table[j] : -1;
+    const T *row = src + (long long)j * kBlk * stride;
+    const bool all_new = tg * 4 >= lo && tg * 4 + 4 <= hi;
+    Raw8<T> raw[4];
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    const int tok = tg * 4 + k;
-    if (tok >= lo && tok < hi) load8(src + (first + k) * stride, f[k]);
-    else {
+    for (int k = 0; k < 4; ++k) {
+      const bool is_new = all_new || (tg * 4 + k >= lo && tg * 4 + k < hi);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) f[k][i] = 0.f;
+      for (int i = 0; i < (int)sizeof(T) / 2; ++i) raw[k].v[i] = is_new ? reinterpret_cast<const uint4 *>(row + k * stride)[i] : make_uint4(0u, 0u, 0u, 0u);
     }
-  }
-#pragma unroll
-  for (int k = 0; k < 4; ++k)
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const uint32_t m = __float_as_uint(f[k][i]) & 0x7fffffffu;
-      amax = max(amax, m < 0x7f800000u ? m : 0u);                                 // infinities and NaN set no scale
+    if (id < 0 || id >= a.n_blocks) {                                             // the same in all threads
+      if (threadIdx.x == 0 && a.status) *a.status = PD_ERR_ARG;
+      continue;
     }
-  __shared__ uint32_t warp_max[8];
-  amax = __reduce_max_sync(0xffffffffu, amax);
-  if ((threadIdx.x & 31) == 0) warp_max[threadIdx.x >> 5] = amax;
-  __syncthreads();
+    const size_t part = ((size_t)id * a.heads + h) * 2 + is_v;
+    const float had = lo > 0 ? a.scales[part] : 0.f;
+    typename AbsMaxOf<T>::type most;
 #pragma unroll
-  for (int w = 0; w < 4; ++w) amax = max(amax, warp_max[is_v * 4 + w]);
-  const float fresh = pow2(scale_exponent(amax)), scale = fmaxf(fresh, had);
-  const float inv = 1.f / scale;                                                  // exact: a power of two
-  uint8_t *dst = a.codes + part * kPart;
-  if (lo > 0 && scale > had) {                                                    // older tokens of the block move to the new scale
-    const float g = had * inv;
-    if (!is_v) {
-      for (int w = t; w < lo * (kDh / 4); w += 128) {
-        uint32_t *p = reinterpret_cast<uint32_t *>(dst) + w;
-        *p = rescale4(*p, g);
-      }
-    } else {
-      for (int w = t; w < kDh * kBlk / 4; w += 128) {
-        const int tok = (w & 15) * 4;
-        if (tok >= lo) continue;
-        uint32_t *p = reinterpret_cast<uint32_t *>(dst) + w;
-        const uint32_t r = rescale4(*p, g);
-        if (tok + 4 <= lo) *p = r;
-        else                                                                      // the word's other bytes are new tokens'
-          for (int k = 0; k < lo - tok; ++k) reinterpret_cast<uint8_t *>(p)[k] = (uint8_t)(r >> (8 * k));
-      }
-    }
-  }
-  if (tg * 4 + 4 > lo && tg * 4 < hi) {
-    if (!is_v) {
+    for (int k = 0; k < 4; ++k) most.add(raw[k]);
+    uint32_t amax = __reduce_max_sync(0xffffffffu, most.bits());
+    if ((threadIdx.x & 31) == 0) warp_max[turn][warp] = amax;
+    if (__syncthreads_or(amax >= 0x7f800000u)) {                                  // infinities set no scale: once more without them
+      amax = 0;
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        const int tok = tg * 4 + k;
-        if (tok >= lo && tok < hi)
-          *reinterpret_cast<uint2 *>(dst + tok * kDh + dg * 8) =
-              make_uint2(e4m3x4(f[k][0] * inv, f[k][1] * inv, f[k][2] * inv, f[k][3] * inv), e4m3x4(f[k][4] * inv, f[k][5] * inv, f[k][6] * inv, f[k][7] * inv));
+        float f[8];
+        unpack8(raw[k], f);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const uint32_t m = __float_as_uint(f[i]) & 0x7fffffffu;
+          amax = max(amax, m < 0x7f800000u ? m : 0u);
+        }
       }
-    } else {
-      const bool whole = tg * 4 >= lo && tg * 4 + 4 <= hi;
+      amax = __reduce_max_sync(0xffffffffu, amax);
+      __syncthreads();
+      if ((threadIdx.x & 31) == 0) warp_max[turn][warp] = amax;
+      __syncthreads();
+    }
+    amax = 0;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const uint32_t w = e4m3x4(f[0][i] * inv, f[1][i] * inv, f[2][i] * inv, f[3][i] * inv);
-        uint8_t *p = dst + (dg * 8 + i) * kBlk + tg * 4;
-        if (whole) *reinterpret_cast<uint32_t *>(p) = w;
-        else {
-#pragma unroll
-          for (int k = 0; k < 4; ++k)
-            if (tg * 4 + k >= lo && tg * 4 + k < hi) p[k] = (uint8_t)(w >> (8 * k));
+    for (int w = 0; w < 4; ++w) amax = max(amax, warp_max[turn][w]);
+    const float scale = fmaxf(pow2(scale_exponent(amax)), had);
+    const float inv = 1.f / scale;                                                // exact: a power of two
+    uint8_t *dst = a.codes + part * kPart;
+    if (lo > 0 && scale > had) {                                                  // older tokens of the block move to the new scale
+      const float g = had * inv;
+      if (!is_v) {
+        for (int w = t; w < lo * (kDh / 4); w += 128) {
+          uint32_t *p = reinterpret_cast<uint32_t *>(dst) + w;
+          *p = rescale4(*p, g);
+        }
+      } else {
+        for (int w = t; w < kDh * kBlk / 4; w += 128) {
+          const int tok = (w & 15) * 4;
+          if (tok >= lo) continue;
+          uint32_t *p = reinterpret_cast<uint32_t *>(dst) + w;
+          const uint32_t r = rescale4(*p, g);
+          if (tok + 4 <= lo) *p = r;
+          else                                                                    // the word's other bytes are new tokens'
+            for (int k = 0; k < lo - tok; ++k) reinterpret_cast<uint8_t *>(p)[k] = (uint8_t)(r >> (8 * k));
         }
       }
     }
+    if (tg * 4 + 4 > lo && tg * 4 < hi) {
+      float f[4][8];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        unpack8(raw[k], f[k]);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[k][i] *= inv;
+      }
+      if (!is_v) {
+        uint8_t *p = dst + tg * 4 * kDh + dg * 8;
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          if (all_new || (tg * 4 + k >= lo && tg * 4 + k < hi))
+            *reinterpret_cast<uint2 *>(p + k * kDh) = make_uint2(e4m3x4(f[k][0], f[k][1], f[k][2], f[k][3]), e4m3x4(f[k][4], f[k][5], f[k][6], f[k][7]));
+      } else {
+        uint8_t *p = dst + dg * 8 * kBlk + tg * 4;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const uint32_t w = e4m3x4(f[0][i], f[1][i], f[2][i], f[3][i]);
+          if (all_new) *reinterpret_cast<uint32_t *>(p + i * kBlk) = w;
+          else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              if (tg * 4 + k >= lo && tg * 4 + k < hi) p[i * kBlk + k] = (uint8_t)(w >> (8 * k));
+          }
+        }
+      }
+    }
+    if (t == 0) a.scales[part] = scale;
   }
-  if (t == 0) a.scales[part] = scale;
 }
 
 }  // namespace
@@ -182,9 +236,10 @@ extern "C" pd_status pd_cache_append(int32_t dtype, int32_t batch, int32_t n_kv_
   a.k = k; a.v = v; a.k_stride = k_stride; a.v_stride = v_stride;
   a.row_start = row_start; a.n_new = n_new; a.pos_start = pos_start; a.table = table;
   a.codes = static_cast<uint8_t *>(codes); a.scales = scales; a.status = status;
-  // blocks that max_new tokens touch at most, wherever they begin
-  const dim3 grid((unsigned)(((long long)max_new + kBlk - 2) / kBlk + 1), n_kv_heads, batch);
+  // blocks that max_new tokens touch at most, wherever they begin; a CTA walks several where there are more than keep the GPU busy
+  const long long blocks = ((long long)max_new + kBlk - 2) / kBlk + 1, pairs = (long long)n_kv_heads * batch;
+  const dim3 grid(2 * n_kv_heads, (unsigned)std::min(65535ll, std::max(1ll, std::min(blocks, kAppendCtas / pairs))), batch);
   cudaStream_t s = reinterpret_cast<cudaStream_t>(cuda_stream);
-  const cudaError_t st = op_launch(dtype == PD_DTYPE_BF16 ? cache_append_kernel<__nv_bfloat16> : cache_append_kernel<float>, grid, 256, 0, 1, s, a);
+  const cudaError_t st = op_launch(dtype == PD_DTYPE_BF16 ? cache_append_kernel<__nv_bfloat16> : cache_append_kernel<float>, grid, 128, 0, 1, s, a);
   return st == cudaSuccess ? PD_OK : PD_ERR_CUDA;
 }

@@ -19,6 +19,7 @@ namespace {
 
 constexpr int kRotThreads = 256;
 constexpr int kRotMaxTokens = 8;         // tokens per CTA
+constexpr int kBatch = 4;                // tokens whose loads a thread has under way together
 constexpr int kRotMaxHead = 256;
 
 struct RotaryArgs {
@@ -29,73 +30,141 @@ struct RotaryArgs {
   int tokens, heads, dh, rot, inverse, copy_rest, tok_per_cta;
 };
 
-template <typename T> __device__ __forceinline__ float to_f(T v);
-template <> __device__ __forceinline__ float to_f(float v) { return v; }
-template <> __device__ __forceinline__ float to_f(__nv_bfloat16 v) { return __bfloat162float(v); }
-template <typename T> __device__ __forceinline__ T of_f(float v);
-template <> __device__ __forceinline__ float of_f(float v) { return v; }
-template <> __device__ __forceinline__ __nv_bfloat16 of_f(float v) { return __float2bfloat16_rn(v); }
+// What one access moves, as it lies in memory and as numbers.
+template <typename T, int VEC> struct Piece;
+template <> struct Piece<float, 4> {
+  float4 v;
+  __device__ __forceinline__ void unpack(float (&f)[4]) const { f[0] = v.x; f[1] = v.y; f[2] = v.z; f[3] = v.w; }
+  __device__ __forceinline__ void pack(const float (&f)[4]) { v = make_float4(f[0], f[1], f[2], f[3]); }
+};
+template <> struct Piece<__nv_bfloat16, 8> {
+  uint4 v;
+  __device__ __forceinline__ void unpack(float (&f)[8]) const {
+    const uint32_t u[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { f[2 * i] = __uint_as_float(u[i] << 16); f[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u); }
+  }
+  __device__ __forceinline__ void pack(const float (&f)[8]) {
+    uint32_t u[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const __nv_bfloat162 b = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
+      u[i] = *reinterpret_cast<const uint32_t *>(&b);
+    }
+    v = make_uint4(u[0], u[1], u[2], u[3]);
+  }
+};
+template <> struct Piece<float, 1> {
+  float v;
+  __device__ __forceinline__ void unpack(float (&f)[1]) const { f[0] = v; }
+  __device__ __forceinline__ void pack(const float (&f)[1]) { v = f[0]; }
+};
+template <> struct Piece<__nv_bfloat16, 1> {
+  __nv_bfloat16 v;
+  __device__ __forceinline__ void unpack(float (&f)[1]) const { f[0] = __bfloat162float(v); }
+  __device__ __forceinline__ void pack(const float (&f)[1]) { v = __float2bfloat16_rn(f[0]); }
+};
 
-template <typename T, int N> struct alignas(sizeof(T) * N) Vec { T v[N]; };
+// u c + v s, written out so that every form of the kernel gives the same bits.
+__device__ __forceinline__ float turned(float u, float c, float v, float s) { return fmaf(u, c, __fmul_rn(v, s)); }
 
-// VEC elements per access: 16 bytes, or 1 where the shape, the strides or the addresses do not allow it.
+// VEC elements per access: 16 bytes, or 1 where the shape, the strides or the addresses do not allow it.  An item is what one thread
+// turns of a head at a time - VEC pairs (halves), VEC / 2 pairs (neighbours), one pair where VEC is 1 - or copies of its rest.  A thread
+// keeps its item (or one every 256) and takes it of several tokens at once: loads of kBatch tokens are under way together, the first ones
+// while sines and cosines are computed.
 template <typename T, bool INTERLEAVED, int VEC>
-__global__ void __launch_bounds__(kRotThreads) rotary_kernel(RotaryArgs a) {
+__global__ void __launch_bounds__(kRotThreads, 4) rotary_kernel(RotaryArgs a) {
   __shared__ float2 cs[kRotMaxTokens * kRotMaxHead / 2];
   op_begin();
-  const int half = a.rot / 2, tok0 = blockIdx.x * a.tok_per_cta;
-  const int nt = min(a.tok_per_cta, a.tokens - tok0);
-  for (int i = threadIdx.x; i < nt * half; i += kRotThreads) {
+  using V = Piece<T, VEC>;
+  constexpr bool TWO = !(INTERLEAVED && VEC > 1);                      // an item is two pieces of a head
+  constexpr int PAIRS = VEC == 1 ? 1 : INTERLEAVED ? VEC / 2 : VEC;
+  const int half = a.rot / 2, tok0 = blockIdx.x * a.tok_per_cta, nt = min(a.tok_per_cta, a.tokens - tok0);
+  const int turn_items = half / PAIRS, items = turn_items + (a.copy_rest ? (a.dh - a.rot) / VEC : 0), per_tok = items * a.heads;
+  const int threads = blockDim.x, groups = max(threads / per_tok, 1), grp = groups > 1 ? threadIdx.x / per_tok : 0;      // groups of threads that share the tokens
+  const int step = groups > 1 ? per_tok : threads, r0 = threadIdx.x - grp * step;
+  const int per_item = grp < groups ? (nt - grp + groups * kBatch - 1) / (groups * kBatch) : 0;       // batches of an item
+  const int n = r0 < per_tok ? (per_tok - r0 + step - 1) / step * per_item : 0;
+  V pa[kBatch], pb[kBatch];
+  int at_a = 0, at_b = 0, at_cs = 0, tt0 = 0, h = 0, r = r0, batch = -1;
+  bool turn = false;
+  auto load = [&] {                                                     // the next batch
+    if (++batch == per_item) { batch = 0; r += step; }
+    if (batch == 0) {
+      h = r / items;
+      const int c = r - h * items;
+      turn = c < turn_items;
+      at_cs = c * PAIRS;
+      at_a = !turn ? a.rot + (c - turn_items) * VEC : VEC > 1 ? c * VEC : INTERLEAVED ? 2 * c : c;
+      at_b = INTERLEAVED ? at_a + 1 : at_a + half;
+    }
+    tt0 = grp + batch * groups * kBatch;
+    const T *x = static_cast<const T *>(a.x) + h * a.x_head;
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) {
+      const int tt = tt0 + k * groups;
+      if (tt < nt) {
+        const T *p = x + (tok0 + tt) * a.x_tok;
+        pa[k] = *reinterpret_cast<const V *>(p + at_a);
+        if (TWO && turn) pb[k] = *reinterpret_cast<const V *>(p + at_b);
+      }
+    }
+  };
+  if (n > 0) load();
+  for (int i = threadIdx.x; i < nt * half; i += threads) {
     const double t = (double)a.pos[tok0 + i / half] * a.turns[i % half];
     float s, c;
     sincospif((float)(2.0 * (t - rint(t))), &s, &c);
     cs[i] = make_float2(c * a.amplitude, (a.inverse ? -s : s) * a.amplitude);
   }
   __syncthreads();
-  using V = Vec<T, VEC>;
-  // items of a head: VEC pairs (halves) or VEC / 2 pairs (neighbours) each - one pair where VEC is 1 -, then the rest of the head
-  constexpr int PAIRS = VEC == 1 ? 1 : INTERLEAVED ? VEC / 2 : VEC;
-  const int turn_items = half / PAIRS, items = turn_items + (a.copy_rest ? (a.dh - a.rot) / VEC : 0);
-  const int per_tok = items * a.heads, total = nt * per_tok;
-#pragma unroll 4
-  for (int i = threadIdx.x; i < total; i += kRotThreads) {
-    const int tt = i / per_tok, r = i - tt * per_tok, h = r / items, c = r - h * items;
-    const T *x = static_cast<const T *>(a.x) + (tok0 + tt) * a.x_tok + h * a.x_head;
-    T *o = static_cast<T *>(a.out) + (tok0 + tt) * a.o_tok + h * a.o_head;
-    if (c >= turn_items) {
-      const int at = a.rot + (c - turn_items) * VEC;
-      *reinterpret_cast<V *>(o + at) = *reinterpret_cast<const V *>(x + at);
-      continue;
-    }
-    const float2 *w = cs + tt * half + c * PAIRS;
-    if (INTERLEAVED && VEC > 1) {
-      V p = *reinterpret_cast<const V *>(x + c * VEC);
+  for (int i = 0; i < n; ++i) {
+    if (i) load();
+    T *o = static_cast<T *>(a.out) + h * a.o_head;
 #pragma unroll
-      for (int k = 0; k < VEC / 2; ++k) {
-        const float xa = to_f(p.v[2 * k]), xb = to_f(p.v[2 * k + 1]);
-        p.v[2 * k] = of_f<T>(xa * w[k].x - xb * w[k].y);
-        p.v[2 * k + 1] = of_f<T>(xa * w[k].y + xb * w[k].x);
-      }
-      *reinterpret_cast<V *>(o + c * VEC) = p;
-    } else {
-      const int ia = INTERLEAVED ? 2 * c : c * VEC, ib = INTERLEAVED ? 2 * c + 1 : half + c * VEC;
-      V pa = *reinterpret_cast<const V *>(x + ia), pb = *reinterpret_cast<const V *>(x + ib);
+    for (int k = 0; k < kBatch; ++k) {
+      const int tt = tt0 + k * groups;
+      if (tt >= nt) break;
+      T *p = o + (tok0 + tt) * a.o_tok;
+      const float2 *w = cs + tt * half + at_cs;
+      if (turn) {
+        float x[VEC], y[VEC];
+        pa[k].unpack(x);
+        if (TWO) {
+          pb[k].unpack(y);
 #pragma unroll
-      for (int k = 0; k < VEC; ++k) {
-        const float xa = to_f(pa.v[k]), xb = to_f(pb.v[k]);
-        pa.v[k] = of_f<T>(xa * w[k].x - xb * w[k].y);
-        pb.v[k] = of_f<T>(xa * w[k].y + xb * w[k].x);
+          for (int e = 0; e < VEC; ++e) {
+            const float2 z = w[e];
+            const float xa = x[e], xb = y[e];
+            x[e] = turned(xa, z.x, -xb, z.y);
+            y[e] = turned(xb, z.x, xa, z.y);
+          }
+          pb[k].pack(y);
+          *reinterpret_cast<V *>(p + at_b) = pb[k];
+        } else {
+#pragma unroll
+          for (int e = 0; e < VEC / 2; ++e) {
+            const float2 z = w[e];
+            const float xa = x[2 * e], xb = x[2 * e + 1];
+            x[2 * e] = turned(xa, z.x, -xb, z.y);
+            x[2 * e + 1] = turned(xb, z.x, xa, z.y);
+          }
+        }
+        pa[k].pack(x);
       }
-      *reinterpret_cast<V *>(o + ia) = pa;
-      *reinterpret_cast<V *>(o + ib) = pb;
+      *reinterpret_cast<V *>(p + at_a) = pa[k];
     }
   }
 }
 
 template <typename T, int VEC>
 cudaError_t launch_rotary(const RotaryArgs &a, int interleaved, cudaStream_t s) {
+  const int pairs = VEC == 1 ? 1 : interleaved ? VEC / 2 : VEC;
+  const long long per_tok = ((long long)a.rot / 2 / pairs + (a.copy_rest ? (a.dh - a.rot) / VEC : 0)) * a.heads;
+  // whole groups of a token's items, so that few threads have none
+  const int threads = per_tok >= kRotThreads ? kRotThreads : (int)((kRotThreads / per_tok * per_tok + 31) / 32 * 32);
   const int grid = (a.tokens + a.tok_per_cta - 1) / a.tok_per_cta;
-  return op_launch(interleaved ? rotary_kernel<T, true, VEC> : rotary_kernel<T, false, VEC>, dim3(grid), kRotThreads, 0, 1, s, a);
+  return op_launch(interleaved ? rotary_kernel<T, true, VEC> : rotary_kernel<T, false, VEC>, dim3(grid), threads, 0, 1, s, a);
 }
 
 }  // namespace
