@@ -25,7 +25,7 @@ namespace {
 
 constexpr int kBlk = PD_CACHE_BLOCK;
 constexpr int kPart = kBlk * kDh;                 // codes of a block's keys (values) of one head
-constexpr long long kAppendCtas = 24 * kSms;
+constexpr long long kAppendCtas = 64 * kSms;
 
 struct AppendArgs {
   int heads, n_blocks, max_blocks, rows, max_new;
@@ -103,117 +103,131 @@ template <typename T> struct AbsMaxOf { using type = AbsMax32; };
 template <> struct AbsMaxOf<__nv_bfloat16> { using type = AbsMax16; };
 
 template <typename T>
-__global__ void __launch_bounds__(128, 8) cache_append_kernel(AppendArgs a) {
-  __shared__ uint32_t warp_max[2][4];
+__global__ void __launch_bounds__(128, sizeof(T) == 2 ? 7 : 4) cache_append_kernel(AppendArgs a) {
+  __shared__ uint32_t warp_max[2][2][4];
   op_begin();
-  const int b = blockIdx.z, h = blockIdx.x >> 1, is_v = blockIdx.x & 1, warp = threadIdx.x >> 5, t = threadIdx.x;
+  const int b = blockIdx.z, h = blockIdx.x, warp = threadIdx.x >> 5, t = threadIdx.x;
   const int n = a.n_new[b], p0 = a.pos_start[b], row0 = a.row_start[b];
   if (n <= 0) return;
   if (n > a.max_new || p0 < 0 || row0 < 0 || (long long)row0 + n > a.rows) {
     if (threadIdx.x == 0 && a.status) *a.status = PD_ERR_ARG;
     return;
   }
-  // four tokens of eight dims; keys: neighbouring lanes share a token, values: they share dims
-  const int dg = is_v ? t >> 4 : t & 7, tg = is_v ? t & 15 : t >> 3;
-  const long long stride = is_v ? a.v_stride : a.k_stride, end = (long long)p0 + n;
-  const T *src = static_cast<const T *>(is_v ? a.v : a.k) + h * kDh + dg * 8 + (row0 - (long long)p0 + tg * 4) * stride;     // the four tokens in block 0
+  // four tokens of eight dims, of the keys and of the values; keys: neighbouring lanes share a token, values: they share dims
+  const int dg[2] = {t & 7, t >> 4}, tg[2] = {t >> 3, t & 15};
+  const long long stride[2] = {a.k_stride, a.v_stride}, end = (long long)p0 + n;
+  const T *src[2];                                                                // the thread's first token in block 0
+#pragma unroll
+  for (int w = 0; w < 2; ++w)
+    src[w] = static_cast<const T *>(w ? a.v : a.k) + h * kDh + dg[w] * 8 + (row0 - (long long)p0 + tg[w] * 4) * stride[w];
   const int32_t *table = a.table + (size_t)b * a.max_blocks;
   const int j1 = (int)((end - 1) / kBlk);
   int turn = 0;
   for (int j = p0 / kBlk + blockIdx.y; j <= j1; j += gridDim.y, turn ^= 1) {      // blocks of the sequence
     const int lo = max(p0 - j * kBlk, 0), hi = (int)min(end - (long long)j * kBlk, (long long)kBlk);
     const int id = j < a.max_blocks ? table[j] : -1;
-    const T *row = src + (long long)j * kBlk * stride;
-    const bool all_new = tg * 4 >= lo && tg * 4 + 4 <= hi;
-    Raw8<T> raw[4];
+    auto is_new = [&](int w, int k) { return tg[w] * 4 + k >= lo && tg[w] * 4 + k < hi; };
+    Raw8<T> raw[2][4];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const bool is_new = all_new || (tg * 4 + k >= lo && tg * 4 + k < hi);
+    for (int w = 0; w < 2; ++w) {
+      const T *row = src[w] + (long long)j * kBlk * stride[w];
 #pragma unroll
-      for (int i = 0; i < (int)sizeof(T) / 2; ++i) raw[k].v[i] = is_new ? reinterpret_cast<const uint4 *>(row + k * stride)[i] : make_uint4(0u, 0u, 0u, 0u);
+      for (int k = 0; k < 4; ++k)
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i)
+          raw[w][k].v[i] = is_new(w, k) ? reinterpret_cast<const uint4 *>(row + k * stride[w])[i] : make_uint4(0u, 0u, 0u, 0u);
     }
     if (id < 0 || id >= a.n_blocks) {                                             // the same in all threads
       if (threadIdx.x == 0 && a.status) *a.status = PD_ERR_ARG;
       continue;
     }
-    const size_t part = ((size_t)id * a.heads + h) * 2 + is_v;
-    const float had = lo > 0 ? a.scales[part] : 0.f;
-    typename AbsMaxOf<T>::type most;
+    const size_t block = (size_t)id * a.heads + h;
+    const float2 had = lo > 0 ? reinterpret_cast<const float2 *>(a.scales)[block] : make_float2(0.f, 0.f);
+    uint32_t amax[2];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) most.add(raw[k]);
-    uint32_t amax = __reduce_max_sync(0xffffffffu, most.bits());
-    if ((threadIdx.x & 31) == 0) warp_max[turn][warp] = amax;
-    if (__syncthreads_or(amax >= 0x7f800000u)) {                                  // infinities set no scale: once more without them
-      amax = 0;
+    for (int w = 0; w < 2; ++w) {
+      typename AbsMaxOf<T>::type most;
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        float f[8];
-        unpack8(raw[k], f);
+      for (int k = 0; k < 4; ++k) most.add(raw[w][k]);
+      amax[w] = __reduce_max_sync(0xffffffffu, most.bits());
+      if ((t & 31) == 0) warp_max[turn][w][warp] = amax[w];
+    }
+    if (__syncthreads_or(max(amax[0], amax[1]) >= 0x7f800000u)) {                 // infinities set no scale: once more without them
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const uint32_t m = __float_as_uint(f[i]) & 0x7fffffffu;
-          amax = max(amax, m < 0x7f800000u ? m : 0u);
+      for (int w = 0; w < 2; ++w) {
+        amax[w] = 0;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          float f[8];
+          unpack8(raw[w][k], f);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const uint32_t m = __float_as_uint(f[i]) & 0x7fffffffu;
+            amax[w] = max(amax[w], m < 0x7f800000u ? m : 0u);
+          }
         }
+        amax[w] = __reduce_max_sync(0xffffffffu, amax[w]);
+        if ((t & 31) == 0) warp_max[turn][w][warp] = amax[w];
       }
-      amax = __reduce_max_sync(0xffffffffu, amax);
-      __syncthreads();
-      if ((threadIdx.x & 31) == 0) warp_max[turn][warp] = amax;
       __syncthreads();
     }
-    amax = 0;
+    float scale[2];
 #pragma unroll
-    for (int w = 0; w < 4; ++w) amax = max(amax, warp_max[turn][w]);
-    const float scale = fmaxf(pow2(scale_exponent(amax)), had);
-    const float inv = 1.f / scale;                                                // exact: a power of two
-    uint8_t *dst = a.codes + part * kPart;
-    if (lo > 0 && scale > had) {                                                  // older tokens of the block move to the new scale
-      const float g = had * inv;
-      if (!is_v) {
-        for (int w = t; w < lo * (kDh / 4); w += 128) {
-          uint32_t *p = reinterpret_cast<uint32_t *>(dst) + w;
-          *p = rescale4(*p, g);
-        }
-      } else {
-        for (int w = t; w < kDh * kBlk / 4; w += 128) {
-          const int tok = (w & 15) * 4;
-          if (tok >= lo) continue;
-          uint32_t *p = reinterpret_cast<uint32_t *>(dst) + w;
-          const uint32_t r = rescale4(*p, g);
-          if (tok + 4 <= lo) *p = r;
-          else                                                                    // the word's other bytes are new tokens'
-            for (int k = 0; k < lo - tok; ++k) reinterpret_cast<uint8_t *>(p)[k] = (uint8_t)(r >> (8 * k));
+    for (int w = 0; w < 2; ++w) {
+      const uint32_t m = max(max(warp_max[turn][w][0], warp_max[turn][w][1]), max(warp_max[turn][w][2], warp_max[turn][w][3]));
+      const float held = w ? had.y : had.x;
+      scale[w] = fmaxf(pow2(scale_exponent(m)), held);
+      const float inv = 1.f / scale[w];                                           // exact: a power of two
+      uint8_t *dst = a.codes + (block * 2 + w) * kPart;
+      if (lo > 0 && scale[w] > held) {                                            // older tokens of the block move to the new scale
+        const float g = held * inv;
+        if (w == 0) {
+          for (int i = t; i < lo * (kDh / 4); i += 128) {
+            uint32_t *p = reinterpret_cast<uint32_t *>(dst) + i;
+            *p = rescale4(*p, g);
+          }
+        } else {
+          for (int i = t; i < kDh * kBlk / 4; i += 128) {
+            const int tok = (i & 15) * 4;
+            if (tok >= lo) continue;
+            uint32_t *p = reinterpret_cast<uint32_t *>(dst) + i;
+            const uint32_t r = rescale4(*p, g);
+            if (tok + 4 <= lo) *p = r;
+            else                                                                  // the word's other bytes are new tokens'
+              for (int k = 0; k < lo - tok; ++k) reinterpret_cast<uint8_t *>(p)[k] = (uint8_t)(r >> (8 * k));
+          }
         }
       }
-    }
-    if (tg * 4 + 4 > lo && tg * 4 < hi) {
+      if (tg[w] * 4 + 4 <= lo || tg[w] * 4 >= hi) continue;
       float f[4][8];
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        unpack8(raw[k], f[k]);
+        unpack8(raw[w][k], f[k]);
 #pragma unroll
         for (int i = 0; i < 8; ++i) f[k][i] *= inv;
       }
-      if (!is_v) {
-        uint8_t *p = dst + tg * 4 * kDh + dg * 8;
+      if (w == 0) {
+        uint8_t *p = dst + tg[w] * 4 * kDh + dg[w] * 8;
 #pragma unroll
         for (int k = 0; k < 4; ++k)
-          if (all_new || (tg * 4 + k >= lo && tg * 4 + k < hi))
+          if (is_new(w, k))
             *reinterpret_cast<uint2 *>(p + k * kDh) = make_uint2(e4m3x4(f[k][0], f[k][1], f[k][2], f[k][3]), e4m3x4(f[k][4], f[k][5], f[k][6], f[k][7]));
       } else {
-        uint8_t *p = dst + dg * 8 * kBlk + tg * 4;
+        const bool whole = is_new(w, 0) && is_new(w, 3);
+        uint8_t *p = dst + dg[w] * 8 * kBlk + tg[w] * 4;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          const uint32_t w = e4m3x4(f[0][i], f[1][i], f[2][i], f[3][i]);
-          if (all_new) *reinterpret_cast<uint32_t *>(p + i * kBlk) = w;
+          const uint32_t c = e4m3x4(f[0][i], f[1][i], f[2][i], f[3][i]);
+          if (whole) *reinterpret_cast<uint32_t *>(p + i * kBlk) = c;
           else {
 #pragma unroll
             for (int k = 0; k < 4; ++k)
-              if (tg * 4 + k >= lo && tg * 4 + k < hi) p[i * kBlk + k] = (uint8_t)(w >> (8 * k));
+              if (is_new(w, k)) p[i * kBlk + k] = (uint8_t)(c >> (8 * k));
           }
         }
       }
     }
-    if (t == 0) a.scales[part] = scale;
+    if (t == 0) reinterpret_cast<float2 *>(a.scales)[block] = make_float2(scale[0], scale[1]);
   }
 }
 
@@ -238,7 +252,7 @@ extern "C" pd_status pd_cache_append(int32_t dtype, int32_t batch, int32_t n_kv_
   a.codes = static_cast<uint8_t *>(codes); a.scales = scales; a.status = status;
   // blocks that max_new tokens touch at most, wherever they begin; a CTA walks several where there are more than keep the GPU busy
   const long long blocks = ((long long)max_new + kBlk - 2) / kBlk + 1, pairs = (long long)n_kv_heads * batch;
-  const dim3 grid(2 * n_kv_heads, (unsigned)std::min(65535ll, std::max(1ll, std::min(blocks, kAppendCtas / pairs))), batch);
+  const dim3 grid(n_kv_heads, (unsigned)std::min(65535ll, std::max(1ll, std::min(blocks, kAppendCtas / pairs))), batch);
   cudaStream_t s = reinterpret_cast<cudaStream_t>(cuda_stream);
   const cudaError_t st = op_launch(dtype == PD_DTYPE_BF16 ? cache_append_kernel<__nv_bfloat16> : cache_append_kernel<float>, grid, 128, 0, 1, s, a);
   return st == cudaSuccess ? PD_OK : PD_ERR_CUDA;

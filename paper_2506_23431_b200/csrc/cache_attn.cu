@@ -20,6 +20,7 @@
 #include <limits.h>
 
 #include <algorithm>
+#include <atomic>
 
 #include "op_launch.cuh"
 #include "pd_internal.h"
@@ -107,6 +108,11 @@ __device__ __forceinline__ uint32_t pack_rest(float lo, float hi, uint32_t packe
 __device__ __forceinline__ float ex2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float rcp(float x) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
 __device__ __forceinline__ float quad_max(float v) {
@@ -349,19 +355,39 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(MT, sizeof(T) == 4)) cac
       for (int x = 0; x < 2; ++x) {
         Row &w = row[mt][x];
         const float mul = fmaxf(w.mul * sc.x, FLT_MIN);                              // a zero would make a masked score no number
-        if (MOD) {
-          const int end = notes.span[mt * 16 + x * 8 + g].y;
-          const float *bias = a.bias ? a.bias + (size_t)(kvh * a.G + (tile * ROWS + mt * 16 + x * 8 + g) % a.G) * a.n_bias : nullptr;
+        if (MOD && a.cap_log2e > 0.f) {
 #pragma unroll
           for (int j = 0; j < 8; ++j)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-              float v = s[mt][j][2 * x + e] * mul;
-              const int pos = p0 + 16 * t + 4 * (j >> 1) + 2 * (j & 1) + e;
-              if (a.cap_log2e > 0.f) v = a.cap_log2e * (NP == 2 ? tanhf(v) : 1.f - __fdividef(2.f, 1.f + ex2(v)));
-              if (bias) v += bias[min(max(end - 1 - pos, 0), a.n_bias - 1)] * kLog2e;
-              s[mt][j][2 * x + e] = v;
+              const float v = s[mt][j][2 * x + e] * mul;
+              s[mt][j][2 * x + e] = NP == 2 ? a.cap_log2e * tanhf(v) : fmaf(-2.f * a.cap_log2e, rcp(1.f + ex2(v)), a.cap_log2e);
             }
+        } else if (MOD) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) { s[mt][j][2 * x] *= mul; s[mt][j][2 * x + 1] *= mul; }
+        }
+        if (MOD && a.bias) {
+          // sixteen neighbouring distances, the largest first: near (in the table), far (its last value) or across an end of the table
+          const float *bias = a.bias + (size_t)(kvh * a.G + (tile * ROWS + mt * 16 + x * 8 + g) % a.G) * a.n_bias;
+          const int most = notes.span[mt * 16 + x * 8 + g].y - 1 - p0 - 16 * t;
+          if (__all_sync(0xffffffffu, most - 15 >= a.n_bias - 1)) {
+            const float far = bias[a.n_bias - 1] * kLog2e;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) { s[mt][j][2 * x] += far; s[mt][j][2 * x + 1] += far; }
+          } else if (__all_sync(0xffffffffu, most >= 15 && most < a.n_bias)) {
+            const float *near = bias + most;
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+#pragma unroll
+              for (int e = 0; e < 2; ++e) s[mt][j][2 * x + e] = fmaf(near[-(4 * (j >> 1) + 2 * (j & 1) + e)], kLog2e, s[mt][j][2 * x + e]);
+          } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+#pragma unroll
+              for (int e = 0; e < 2; ++e)
+                s[mt][j][2 * x + e] = fmaf(bias[min(max(most - (4 * (j >> 1) + 2 * (j & 1) + e), 0), a.n_bias - 1)], kLog2e, s[mt][j][2 * x + e]);
+          }
         }
         if (edge) {
           const int2 sp = notes.span[mt * 16 + x * 8 + g];
@@ -638,8 +664,16 @@ template <typename T, int MT>
 cudaError_t launch_cache_attn(const CacheAttnArgs &a, int batch, bool mod, cudaStream_t s) {
   constexpr int smem = smem_bytes(MT, sizeof(T) == 4);
   auto kernel = mod ? cache_attn_kernel<T, MT, true> : cache_attn_kernel<T, MT, false>;
-  cudaError_t st = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  // once per kernel and device: setting it costs as much host time as a third of the launch
+  static std::atomic<uint64_t> ready[2];
+  int dev = 0;
+  cudaError_t st = cudaGetDevice(&dev);
   if (st != cudaSuccess) return st;
+  const uint64_t bit = 1ull << (dev & 63);
+  if (!(ready[mod].load(std::memory_order_relaxed) & bit)) {
+    if ((st = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem)) != cudaSuccess) return st;
+    ready[mod].fetch_or(bit, std::memory_order_relaxed);
+  }
   st = op_launch(kernel, dim3(a.cluster * a.outer, a.HK * a.tiles, batch), kThreads, smem, a.cluster, s, a);
   if (st != cudaSuccess || a.outer == 1) return st;
   const long long n_out = (long long)batch * a.R * a.H;
