@@ -5,7 +5,7 @@
 //   out(row) = softmax over the visible p (begin <= p < end, p < len) of score . v;  zero where nothing is visible
 //
 // Bound by the cache's bytes: 128 per (token, kv head), read once for all rows that share the head.  A segment is a
-// (sequence, kv head, tile of 16 or 32 rows; a row is a (query row, head of the group)); its blocks are split over CTAs, and in a CTA
+// (sequence, kv head, tile of 16 rows; a row is a (query row, head of the group)); its blocks are split over CTAs, and in a CTA
 // over four warps that work alone: each streams its blocks - keys and values of a (block, head) are 8 KB in one piece -
 // through a ring of its own with bulk copies, and reads them with 16-byte loads straight in the order the tensor cores take them, because a contraction does not
 // see the order of its terms:
@@ -34,19 +34,18 @@ constexpr int kPart = kBlk * kDh;                 // codes of a block's keys (va
 constexpr int kWarps = 4, kThreads = kWarps * 32;
 constexpr int kMaxCluster = 8, kClusterSms = 128;
 constexpr int kOuterBlocks = 4;                   // fewest blocks for each warp where a segment is split beyond a cluster
-// CTAs per SM as the registers allow (one 16-row tile 128, two f16 parts 168, two tiles 255), and slots of 4 KB (a block's keys, or its values) in
-// a warp's ring: what then fits the shared memory.
-__host__ __device__ constexpr int ctas_per_sm(int mt, bool f32) { return mt == 2 ? 2 : f32 ? 3 : 4; }
-__host__ __device__ constexpr int slots(int mt, bool f32) { return mt == 2 ? 6 : f32 ? 4 : 3; }
-__host__ __device__ constexpr int ring_bytes(int mt, bool f32) { return kWarps * slots(mt, f32) * kPart; }
+constexpr int kRows = 16;                         // rows of a tile
+// CTAs per SM as the registers allow (128 a thread; two f16 parts 168), and slots of 4 KB (a block's keys, or its values) in a warp's ring: what then fits the
+// shared memory.
+__host__ __device__ constexpr int ctas_per_sm(bool f32) { return f32 ? 3 : 4; }
+__host__ __device__ constexpr int slots(bool f32) { return f32 ? 4 : 3; }
 constexpr int kRec = kDh + 4;                     // a row's partial result: 64 sums, maximum, sum of weights, alignment
-__host__ __device__ constexpr int inbox_bytes(int mt) { return mt * 16 * kRec * (int)sizeof(float); }
+constexpr int kInboxBytes = kRows * kRec * (int)sizeof(float);
 // What a warp looks up rather than holds in registers: scales and ids of two runs of 16 blocks, spans of its rows, its ring's barriers.
 constexpr int kRun = 16;
-template <int MT> struct WarpNotes { float2 scale[2 * kRun]; int id[2 * kRun]; int2 span[MT * 16]; uint64_t bar[8]; };
-__host__ __device__ constexpr int smem_bytes(int mt, bool f32) {
-  return ring_bytes(mt, f32) + inbox_bytes(mt) + kWarps * (int)(mt == 2 ? sizeof(WarpNotes<2>) : sizeof(WarpNotes<1>));
-}
+struct WarpNotes { float2 scale[2 * kRun]; int id[2 * kRun]; int2 span[kRows]; uint64_t bar[4]; };
+__host__ __device__ constexpr int ring_bytes(bool f32) { return kWarps * slots(f32) * kPart; }
+__host__ __device__ constexpr int smem_bytes(bool f32) { return ring_bytes(f32) + kInboxBytes + kWarps * (int)sizeof(WarpNotes); }
 constexpr uint32_t kSpinLimit = 1u << 24;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLift = 15.f;                     // weights are 2^(s - max + kLift): at most 2^15 in f16
@@ -169,15 +168,14 @@ struct Row {
   float m, l;
 };
 
-// T: type of queries and output; MT: 16-row tiles; MOD: cap or bias.  fp32: queries and weights in two f16 parts.
-template <typename T, int MT, bool MOD>
-__global__ void __launch_bounds__(kThreads, ctas_per_sm(MT, sizeof(T) == 4)) cache_attn_kernel(CacheAttnArgs a) {
-  constexpr int NP = sizeof(T) == 4 ? 2 : 1, NS = slots(MT, NP == 2), RING = ring_bytes(MT, NP == 2);
-  constexpr int ROWS = MT * 16;
+// T: type of queries and output; MOD: cap or bias.  fp32: queries and weights in two f16 parts.
+template <typename T, bool MOD>
+__global__ void __launch_bounds__(kThreads, ctas_per_sm(sizeof(T) == 4)) cache_attn_kernel(CacheAttnArgs a) {
+  constexpr int NP = sizeof(T) == 4 ? 2 : 1, NS = slots(NP == 2), RING = ring_bytes(NP == 2);
   extern __shared__ __align__(128) uint8_t ring[];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const int split = blockIdx.x, splits = gridDim.x, kvh = blockIdx.y / a.tiles, tile = blockIdx.y % a.tiles, b = blockIdx.z;
-  WarpNotes<MT> &notes = reinterpret_cast<WarpNotes<MT> *>(ring + RING + inbox_bytes(MT))[warp];
+  WarpNotes &notes = reinterpret_cast<WarpNotes *>(ring + RING + kInboxBytes)[warp];
   const uint32_t slot0 = smem_u32(ring) + warp * NS * kPart, bar0 = smem_u32(notes.bar);
   if (lane == 0) {
     for (int s = 0; s < NS; ++s) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(bar0 + s * 8) : "memory");
@@ -194,11 +192,11 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(MT, sizeof(T) == 4)) cac
   auto share = [&](int n, int k) { const int q = n / splits; return q * k + min(k, n - q * splits); };
   const int guess = share(blocks_most, split), guess_at = guess + warp + lane * kWarps;
   const int rows_here = a.n_rows[b], len_here = a.lens[b], guess_id = guess_at < a.max_blocks ? table[guess_at] : -1;
-  int2 span[2 * MT];
-  Raw16<T> qv[2 * MT];
+  int2 span[2];
+  Raw16<T> qv[2];
 #pragma unroll
-  for (int i = 0; i < 2 * MT; ++i) {
-    const int m = tile * ROWS + (i >> 1) * 16 + (i & 1) * 8 + g, r = m / a.G, h = kvh * a.G + m % a.G;
+  for (int i = 0; i < 2; ++i) {
+    const int m = tile * kRows + i * 8 + g, r = m / a.G, h = kvh * a.G + m % a.G;
     span[i] = make_int2(0, INT_MAX);
 #pragma unroll
     for (int k = 0; k < (int)sizeof(T); ++k) qv[i].v[k] = make_uint4(0u, 0u, 0u, 0u);
@@ -213,12 +211,12 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(MT, sizeof(T) == 4)) cac
   // ---- the rows and what they see
   const int n_rows = min(max(rows_here, 0), a.R);
   const int len = (int)min((long long)min(max(len_here, 0), a.max_len), (long long)a.max_blocks * kBlk);
-  Row row[MT][2];
+  Row row[2];
   int lo = INT_MAX, hi = 0, all_lo = 0, all_hi = INT_MAX;       // seen by some row; seen by every row that sees anything
 #pragma unroll
-  for (int i = 0; i < 2 * MT; ++i) {
-    Row &w = row[i >> 1][i & 1];
-    const int r = (tile * ROWS + (i >> 1) * 16 + (i & 1) * 8 + g) / a.G;
+  for (int i = 0; i < 2; ++i) {
+    Row &w = row[i];
+    const int r = (tile * kRows + i * 8 + g) / a.G;
     int2 sp = make_int2(0, 0);                                  // begin == end: the row sees nothing
     w.m = -INFINITY; w.l = 0.f;
     if (r < n_rows) {
@@ -252,10 +250,10 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(MT, sizeof(T) == 4)) cac
   }
 
   // ---- queries: dims 16 t + 4 s + {0, 1} | {2, 3} of k16 step s; a row is brought to a largest value in [1, 2) so that f16 holds it
-  uint32_t qf[NP][MT][4][4];
+  uint32_t qf[NP][4][4];
 #pragma unroll
-  for (int i = 0; i < 2 * MT; ++i) {
-    Row &w = row[i >> 1][i & 1];
+  for (int i = 0; i < 2; ++i) {
+    Row &w = row[i];
     float f[16];
     unpack16(qv[i], f);
     if (span[i].x == span[i].y) {
@@ -275,17 +273,15 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(MT, sizeof(T) == 4)) cac
       for (int k = 0; k < 2; ++k) {
         const float x = f[4 * s + 2 * k] * down, y = f[4 * s + 2 * k + 1] * down;
         const uint32_t p = pack(x, y);
-        qf[0][i >> 1][s][2 * k + (i & 1)] = p;
-        if (NP == 2) qf[NP - 1][i >> 1][s][2 * k + (i & 1)] = pack_rest(x, y, p);
+        qf[0][s][2 * k + i] = p;
+        if (NP == 2) qf[NP - 1][s][2 * k + i] = pack_rest(x, y, p);
       }
   }
 
   async_copies_land();
-  float o[MT][8][4];
+  float o[8][4];
 #pragma unroll
-  for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-    for (int dn = 0; dn < 8; ++dn) o[mt][dn][0] = o[mt][dn][1] = o[mt][dn][2] = o[mt][dn][3] = 0.f;
+  for (int dn = 0; dn < 8; ++dn) o[dn][0] = o[dn][1] = o[dn][2] = o[dn][3] = 0.f;
 
   // ---- the blocks
   bool ok = true;
@@ -318,7 +314,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(MT, sizeof(T) == 4)) cac
     const bool edge = p0 < all_lo || p0 + kBlk > all_hi;                           // some row does not see all of it
     if (!(ok = arrived())) break;
     // ---- scores, four tiles of eight tokens at a time: products in a row are independent
-    float s[MT][8][4];
+    float s[8][4];
     const uint32_t kbase = slot0 + st * kPart;
 #pragma unroll
     for (int jh = 0; jh < 8; jh += 4) {
@@ -336,110 +332,101 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(MT, sizeof(T) == 4)) cac
           uint32_t b0, b1;
           widen(u[j][k], b0, b1);
 #pragma unroll
-          for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-            for (int p = 0; p < NP; ++p) {
-              if (k + p == 0) mma_f16_first(s[mt][jh + j], qf[p][mt][k], b0, b1);
-              else mma_f16(s[mt][jh + j], qf[p][mt][k], b0, b1);
-            }
+          for (int p = 0; p < NP; ++p) {
+            if (k + p == 0) mma_f16_first(s[jh + j], qf[p][k], b0, b1);
+            else mma_f16(s[jh + j], qf[p][k], b0, b1);
+          }
         }
     }
     refill(i, 2 * i);
     // ---- the block's softmax; without cap and bias the scale (positive) comes in with the exponent
-    uint32_t pf[NP][MT][4][4];
-    float keep[MT][2], take[MT][2];                                                // factors of the values so far and of this block's
-    float mref[MT][2];
+    uint32_t pf[NP][4][4];
+    float keep[2], take[2];                                                // factors of the values so far and of this block's
+    float mref[2];
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt)
+    for (int x = 0; x < 2; ++x) {
+      Row &w = row[x];
+      const float mul = fmaxf(w.mul * sc.x, FLT_MIN);                              // a zero would make a masked score no number
+      if (MOD && a.cap_log2e > 0.f) {
 #pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        Row &w = row[mt][x];
-        const float mul = fmaxf(w.mul * sc.x, FLT_MIN);                              // a zero would make a masked score no number
-        if (MOD && a.cap_log2e > 0.f) {
+        for (int j = 0; j < 8; ++j)
 #pragma unroll
-          for (int j = 0; j < 8; ++j)
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              const float v = s[mt][j][2 * x + e] * mul;
-              s[mt][j][2 * x + e] = NP == 2 ? a.cap_log2e * tanhf(v) : fmaf(-2.f * a.cap_log2e, rcp(1.f + ex2(v)), a.cap_log2e);
-            }
-        } else if (MOD) {
-#pragma unroll
-          for (int j = 0; j < 8; ++j) { s[mt][j][2 * x] *= mul; s[mt][j][2 * x + 1] *= mul; }
-        }
-        if (MOD && a.bias) {
-          // sixteen neighbouring distances, the largest first: near (in the table), far (its last value) or across an end of the table
-          const float *bias = a.bias + (size_t)(kvh * a.G + (tile * ROWS + mt * 16 + x * 8 + g) % a.G) * a.n_bias;
-          const int most = notes.span[mt * 16 + x * 8 + g].y - 1 - p0 - 16 * t;
-          if (__all_sync(0xffffffffu, most - 15 >= a.n_bias - 1)) {
-            const float far = bias[a.n_bias - 1] * kLog2e;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) { s[mt][j][2 * x] += far; s[mt][j][2 * x + 1] += far; }
-          } else if (__all_sync(0xffffffffu, most >= 15 && most < a.n_bias)) {
-            const float *near = bias + most;
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-#pragma unroll
-              for (int e = 0; e < 2; ++e) s[mt][j][2 * x + e] = fmaf(near[-(4 * (j >> 1) + 2 * (j & 1) + e)], kLog2e, s[mt][j][2 * x + e]);
-          } else {
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-#pragma unroll
-              for (int e = 0; e < 2; ++e)
-                s[mt][j][2 * x + e] = fmaf(bias[min(max(most - (4 * (j >> 1) + 2 * (j & 1) + e), 0), a.n_bias - 1)], kLog2e, s[mt][j][2 * x + e]);
+          for (int e = 0; e < 2; ++e) {
+            const float v = s[j][2 * x + e] * mul;
+            s[j][2 * x + e] = NP == 2 ? a.cap_log2e * tanhf(v) : fmaf(-2.f * a.cap_log2e, rcp(1.f + ex2(v)), a.cap_log2e);
           }
-        }
-        if (edge) {
-          const int2 sp = notes.span[mt * 16 + x * 8 + g];
+      } else if (MOD) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) { s[j][2 * x] *= mul; s[j][2 * x + 1] *= mul; }
+      }
+      if (MOD && a.bias) {
+        // sixteen neighbouring distances, the largest first: near (in the table), far (its last value) or across an end of the table
+        const float *bias = a.bias + (size_t)(kvh * a.G + (tile * kRows + x * 8 + g) % a.G) * a.n_bias;
+        const int most = notes.span[x * 8 + g].y - 1 - p0 - 16 * t;
+        if (__all_sync(0xffffffffu, most - 15 >= a.n_bias - 1)) {
+          const float far = bias[a.n_bias - 1] * kLog2e;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) { s[j][2 * x] += far; s[j][2 * x + 1] += far; }
+        } else if (__all_sync(0xffffffffu, most >= 15 && most < a.n_bias)) {
+          const float *near = bias + most;
 #pragma unroll
           for (int j = 0; j < 8; ++j)
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              const int pos = p0 + 16 * t + 4 * (j >> 1) + 2 * (j & 1) + e;
-              if (pos < sp.x || pos >= sp.y) s[mt][j][2 * x + e] = -INFINITY;
-            }
-        }
-        float mx = -INFINITY;
+            for (int e = 0; e < 2; ++e) s[j][2 * x + e] = fmaf(near[-(4 * (j >> 1) + 2 * (j & 1) + e)], kLog2e, s[j][2 * x + e]);
+        } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) mx = fmaxf(mx, fmaxf(s[mt][j][2 * x], s[mt][j][2 * x + 1]));
-        mx = quad_max(mx);
-        if (!here) mx = -INFINITY;
-        const float f = MOD ? 1.f : mul;
-        mx *= f;
-        const float ref = kLift - (mx == -INFINITY ? 0.f : mx);
+          for (int j = 0; j < 8; ++j)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const float w0 = ex2(MOD ? s[mt][j][2 * x] + ref : fmaf(s[mt][j][2 * x], f, ref)), w1 = ex2(MOD ? s[mt][j][2 * x + 1] + ref : fmaf(s[mt][j][2 * x + 1], f, ref));
-          const uint32_t p = pack(w0, w1);
-          pf[0][mt][j >> 1][2 * (j & 1) + x] = p;
-          if (NP == 2) pf[NP - 1][mt][j >> 1][2 * (j & 1) + x] = pack_rest(w0, w1, p);
+            for (int e = 0; e < 2; ++e)
+              s[j][2 * x + e] = fmaf(bias[min(max(most - (4 * (j >> 1) + 2 * (j & 1) + e), 0), a.n_bias - 1)], kLog2e, s[j][2 * x + e]);
         }
-        const float m_new = fmaxf(w.m, mx);
-        mref[mt][x] = m_new == -INFINITY ? 0.f : m_new;
-        keep[mt][x] = ex2(w.m - mref[mt][x]);
-        take[mt][x] = ex2(mx - mref[mt][x]);
-        w.m = m_new;
       }
+      if (edge) {
+        const int2 sp = notes.span[x * 8 + g];
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const int pos = p0 + 16 * t + 4 * (j >> 1) + 2 * (j & 1) + e;
+            if (pos < sp.x || pos >= sp.y) s[j][2 * x + e] = -INFINITY;
+          }
+      }
+      float mx = -INFINITY;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) mx = fmaxf(mx, fmaxf(s[j][2 * x], s[j][2 * x + 1]));
+      mx = quad_max(mx);
+      if (!here) mx = -INFINITY;
+      const float f = MOD ? 1.f : mul;
+      mx *= f;
+      const float ref = kLift - (mx == -INFINITY ? 0.f : mx);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float w0 = ex2(MOD ? s[j][2 * x] + ref : fmaf(s[j][2 * x], f, ref)), w1 = ex2(MOD ? s[j][2 * x + 1] + ref : fmaf(s[j][2 * x + 1], f, ref));
+        const uint32_t p = pack(w0, w1);
+        pf[0][j >> 1][2 * (j & 1) + x] = p;
+        if (NP == 2) pf[NP - 1][j >> 1][2 * (j & 1) + x] = pack_rest(w0, w1, p);
+      }
+      const float m_new = fmaxf(w.m, mx);
+      mref[x] = m_new == -INFINITY ? 0.f : m_new;
+      keep[x] = ex2(w.m - mref[x]);
+      take[x] = ex2(mx - mref[x]);
+      w.m = m_new;
+    }
     // ---- values, four tiles of eight dims at a time
     if (!(ok = arrived())) break;
     const uint32_t vbase = slot0 + st * kPart;
-    bool moved = false;                                                            // some row's running maximum did
+    if (__any_sync(0xffffffffu, keep[0] != 1.f || keep[1] != 1.f)) {               // some row's running maximum moved
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt) moved |= keep[mt][0] != 1.f || keep[mt][1] != 1.f;
-    if (__any_sync(0xffffffffu, moved)) {
+      for (int dn = 0; dn < 8; ++dn)
 #pragma unroll
-      for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-        for (int dn = 0; dn < 8; ++dn)
-#pragma unroll
-          for (int x = 0; x < 4; ++x) o[mt][dn][x] *= keep[mt][x >> 1];
+        for (int x = 0; x < 4; ++x) o[dn][x] *= keep[x >> 1];
     }
     uint32_t nan_seen = 0;                                                         // values that are no numbers, at positions that some row sees
     if (here) {
 #pragma unroll
       for (int dh = 0; dh < 8; dh += 4) {
         uint32_t u[4][4];
-        float tv[MT][4][4];
+        float tv[4][4];
 #pragma unroll
         for (int dn = 0; dn < 4; ++dn) {
           const uint4 w = lds128(vbase + ((dh + dn) * 8 + g) * kBlk + t * 16);
@@ -465,65 +452,55 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(MT, sizeof(T) == 4)) cac
             uint32_t b0, b1;
             widen(u[dn][k], b0, b1);
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-              for (int p = 0; p < NP; ++p) {
-                if (k + p == 0) mma_f16_first(tv[mt][dn], pf[p][mt][k], b0, b1);
-                else mma_f16(tv[mt][dn], pf[p][mt][k], b0, b1);
-              }
+            for (int p = 0; p < NP; ++p) {
+              if (k + p == 0) mma_f16_first(tv[dn], pf[p][k], b0, b1);
+              else mma_f16(tv[dn], pf[p][k], b0, b1);
+            }
           }
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
+        for (int dn = 0; dn < 4; ++dn)
 #pragma unroll
-          for (int dn = 0; dn < 4; ++dn)
-#pragma unroll
-            for (int x = 0; x < 4; ++x) o[mt][dh + dn][x] = fmaf(tv[mt][dn][x], take[mt][x >> 1] * sc.y, o[mt][dh + dn][x]);
+          for (int x = 0; x < 4; ++x) o[dh + dn][x] = fmaf(tv[dn][x], take[x >> 1] * sc.y, o[dh + dn][x]);
       }
       if (edge && __any_sync(0xffffffffu, nan_seen != 0)) {
         // rows that see such a value get it after all: a product of who sees which position with where they stand
+        uint32_t sees[4][4];
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
-          uint32_t sees[4][4];
+        for (int x = 0; x < 2; ++x) {
+          const int2 sp = notes.span[x * 8 + g];
 #pragma unroll
-          for (int x = 0; x < 2; ++x) {
-            const int2 sp = notes.span[mt * 16 + x * 8 + g];
+          for (int k = 0; k < 4; ++k)
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
-#pragma unroll
-              for (int y = 0; y < 2; ++y) {
-                const int p = p0 + 16 * t + 4 * k + 2 * y;
-                sees[k][2 * y + x] = (p >= sp.x && p < sp.y ? 0x3c00u : 0u) | (p + 1 >= sp.x && p + 1 < sp.y ? 0x3c000000u : 0u);
-              }
-          }
-#pragma unroll
-          for (int dn = 0; dn < 8; ++dn) {
-            const uint4 w = lds128(vbase + (dn * 8 + g) * kBlk + t * 16);
-            const uint32_t u[4] = {w.x, w.y, w.z, w.w};
-            float c[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              const uint32_t nb = nan_bytes(u[k]);
-              mma_f16(c, sees[k], (nb & 0x80u ? 0x3c00u : 0u) | (nb & 0x8000u ? 0x3c000000u : 0u),
-                      (nb & 0x800000u ? 0x3c00u : 0u) | (nb & 0x80000000u ? 0x3c000000u : 0u));
+            for (int y = 0; y < 2; ++y) {
+              const int p = p0 + 16 * t + 4 * k + 2 * y;
+              sees[k][2 * y + x] = (p >= sp.x && p < sp.y ? 0x3c00u : 0u) | (p + 1 >= sp.x && p + 1 < sp.y ? 0x3c000000u : 0u);
             }
+        }
 #pragma unroll
-            for (int x = 0; x < 4; ++x)
-              if (c[x] > 0.f) o[mt][dn][x] = __int_as_float(0x7fffffff);
+        for (int dn = 0; dn < 8; ++dn) {
+          const uint4 w = lds128(vbase + (dn * 8 + g) * kBlk + t * 16);
+          const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+          float c[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const uint32_t nb = nan_bytes(u[k]);
+            mma_f16(c, sees[k], (nb & 0x80u ? 0x3c00u : 0u) | (nb & 0x8000u ? 0x3c000000u : 0u),
+                    (nb & 0x800000u ? 0x3c00u : 0u) | (nb & 0x80000000u ? 0x3c000000u : 0u));
           }
+#pragma unroll
+          for (int x = 0; x < 4; ++x)
+            if (c[x] > 0.f) o[dn][x] = __int_as_float(0x7fffffff);
         }
       }
     }
     // the weights' sum is a product with ones: every lane of a row gets it, and numerator and denominator see the same roundings
+    float sum[4];
+    mma_f16_first(sum, pf[0][0], 0x3c003c00u, 0x3c003c00u);
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt) {
-      float sum[4];
-      mma_f16_first(sum, pf[0][mt][0], 0x3c003c00u, 0x3c003c00u);
+    for (int i = 1; i < 4 * NP; ++i) mma_f16(sum, pf[i >> 2][i & 3], 0x3c003c00u, 0x3c003c00u);
 #pragma unroll
-      for (int i = 1; i < 4 * NP; ++i) mma_f16(sum, pf[i >> 2][mt][i & 3], 0x3c003c00u, 0x3c003c00u);
-#pragma unroll
-      for (int x = 0; x < 2; ++x)
-        if (here) row[mt][x].l = row[mt][x].l * keep[mt][x] + sum[2 * x] * take[mt][x];
-    }
+    for (int x = 0; x < 2; ++x)
+      if (here) row[x].l = row[x].l * keep[x] + sum[2 * x] * take[x];
     refill(i, 2 * i + 1);
   }
   if (!ok) {                                                                       // the copies in flight must land before the CTA ends
@@ -533,21 +510,19 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(MT, sizeof(T) == 4)) cac
 
   // ---- join the warps, then the cluster's CTAs, both in their order: a thread takes columns 4 k .. 4 k + 3 and 32 + 4 k .. of a row
   __syncthreads();                                                                 // the rings are free
-  float *rec = reinterpret_cast<float *>(ring), *ml = rec + kWarps * ROWS * kDh;   // [warp][row][64], [warp][row][2]
+  float *rec = reinterpret_cast<float *>(ring), *ml = rec + kWarps * kRows * kDh;   // [warp][row][64], [warp][row][2]
 #pragma unroll
-  for (int mt = 0; mt < MT; ++mt)
+  for (int x = 0; x < 2; ++x) {
+    const int m = warp * kRows + x * 8 + g;
+    const int2 sp = notes.span[x * 8 + g];
+    const bool any = sp.x < sp.y;                          // rows that see nothing went along unmasked
+    if (t == 0) store2(ml + 2 * m, any ? row[x].m : -INFINITY, any ? row[x].l : 0.f);
 #pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      const int m = warp * ROWS + mt * 16 + x * 8 + g;
-      const int2 sp = notes.span[mt * 16 + x * 8 + g];
-      const bool any = sp.x < sp.y;                          // rows that see nothing went along unmasked
-      if (t == 0) store2(ml + 2 * m, any ? row[mt][x].m : -INFINITY, any ? row[mt][x].l : 0.f);
-#pragma unroll
-      for (int dn = 0; dn < 8; ++dn)
-        store2(rec + m * kDh + ((dn * 8 + 2 * t) ^ ((g & 3) << 3)), any ? o[mt][dn][2 * x] : 0.f, any ? o[mt][dn][2 * x + 1] : 0.f);
-    }
+    for (int dn = 0; dn < 8; ++dn)
+      store2(rec + m * kDh + ((dn * 8 + 2 * t) ^ ((g & 3) << 3)), any ? o[dn][2 * x] : 0.f, any ? o[dn][2 * x + 1] : 0.f);
+  }
   __syncthreads();
-  const int cluster = a.cluster, rank = split % cluster, own = ROWS / cluster;     // rank k sums rows k * own .. of the cluster's CTAs
+  const int cluster = a.cluster, rank = split % cluster, own = kRows / cluster;     // rank k sums rows k * own .. of the cluster's CTAs
   float *inbox = reinterpret_cast<float *>(ring + RING);                           // [CTA][row of this rank][kRec]
   // Sum of n partial results of a row; `ml_of` and `o_of` give the addresses of one's (maximum, sum) and first columns.
   auto join = [&](int n, auto ml_of, auto o_of, float2 &h, float4 &x, float4 &y) {
@@ -569,12 +544,12 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(MT, sizeof(T) == 4)) cac
   };
   auto finish = [&](int m, int c, float2 h, float4 x, float4 y) {
     if (a.outer > 1) {
-      float *p = a.part + ((((size_t)b * gridDim.y + blockIdx.y) * a.outer + split / cluster) * ROWS + m) * kRec;
+      float *p = a.part + ((((size_t)b * gridDim.y + blockIdx.y) * a.outer + split / cluster) * kRows + m) * kRec;
       store4(p + c, x); store4(p + c + 32, y);
       if (c == 0) store2(p + kDh, h.x, h.y);
       return;
     }
-    const int gm = tile * ROWS + m, r = gm / a.G, head = kvh * a.G + gm % a.G;
+    const int gm = tile * kRows + m, r = gm / a.G, head = kvh * a.G + gm % a.G;
     if (r >= a.R) return;
     const float inv = h.y == 0.f ? 0.f : 1.f / h.y;                                // nothing seen: zero
     T *p = static_cast<T *>(a.out) + (((size_t)b * a.R + r) * a.H + head) * kDh + c;
@@ -583,12 +558,12 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(MT, sizeof(T) == 4)) cac
   };
   if (cluster > 1) cluster_wait();                                                 // all CTAs of the cluster have begun
 #pragma unroll
-  for (int i = threadIdx.x; i < ROWS * 8; i += kThreads) {
+  for (int i = threadIdx.x; i < kRows * 8; i += kThreads) {
     const int m = i >> 3, c = (i & 7) * 4;
     float2 h;
     float4 x, y;
-    join(kWarps, [&](int k) { return reinterpret_cast<const float2 *>(ml + 2 * (k * ROWS + m)); },
-         [&](int k, int at) { return rec + (k * ROWS + m) * kDh + ((c + at) ^ ((m & 3) << 3)); }, h, x, y);
+    join(kWarps, [&](int k) { return reinterpret_cast<const float2 *>(ml + 2 * (k * kRows + m)); },
+         [&](int k, int at) { return rec + (k * kRows + m) * kDh + ((c + at) ^ ((m & 3) << 3)); }, h, x, y);
     if (cluster == 1) { finish(m, c, h, x, y); continue; }
     const uint32_t to = peer_addr(smem_u32(inbox + ((size_t)rank * own + m % own) * kRec), m / own);
     peer_st4(to + c * 4, x); peer_st4(to + (c + 32) * 4, y);
@@ -609,41 +584,51 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(MT, sizeof(T) == 4)) cac
 
 // Joins the splits of a row in their order: one warp per (sequence, row, head), two columns per lane.
 template <typename T>
-__global__ void __launch_bounds__(128) cache_attn_merge_kernel(CacheAttnArgs a, int rows_tile, long long n_out) {
+__global__ void __launch_bounds__(128) cache_attn_merge_kernel(CacheAttnArgs a, long long n_out) {
   op_begin();
   const long long i = (long long)blockIdx.x * 4 + (threadIdx.x >> 5);
   const int lane = threadIdx.x & 31;
   if (i >= n_out) return;
   const int h = (int)(i % a.H), r = (int)(i / a.H % a.R), b = (int)(i / a.H / a.R);
-  const int kvh = h / a.G, m = r * a.G + h % a.G, tile = m / rows_tile;
-  const float *p = a.part + (((size_t)b * a.HK + kvh) * a.tiles + tile) * a.outer * rows_tile * kRec + (size_t)(m % rows_tile) * kRec;
-  const size_t step = (size_t)rows_tile * kRec;
-  float mx = -INFINITY;
-  for (int s = lane; s < a.outer; s += 32) mx = fmaxf(mx, p[s * step + kDh]);
-  for (int x = 16; x; x >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, x));
-  const float ref = mx == -INFINITY ? 0.f : mx;
-  float l = 0.f, x = 0.f, y = 0.f;
-  for (int s = 0; s < a.outer; ++s) {
-    const float2 ml = *reinterpret_cast<const float2 *>(p + s * step + kDh), v = *reinterpret_cast<const float2 *>(p + s * step + 2 * lane);
-    const float f = ex2(ml.x - ref);
-    l += ml.y * f; x += v.x * f; y += v.y * f;
+  const int kvh = h / a.G, m = r * a.G + h % a.G, tile = m / kRows;
+  const float *p = a.part + (((size_t)b * a.HK + kvh) * a.tiles + tile) * a.outer * kRows * kRec + (size_t)(m % kRows) * kRec;
+  const size_t step = (size_t)kRows * kRec;
+  float mx = -INFINITY, l = 0.f, x = 0.f, y = 0.f;
+  for (int s0 = 0; s0 < a.outer; s0 += 8) {                                        // eight splits' loads under way together
+    float2 ml[8], v[8];
+#pragma unroll
+    for (int s = 0; s < 8; ++s) {
+      const bool in = s0 + s < a.outer;
+      ml[s] = in ? *reinterpret_cast<const float2 *>(p + (s0 + s) * step + kDh) : make_float2(-INFINITY, 0.f);
+      v[s] = in ? *reinterpret_cast<const float2 *>(p + (s0 + s) * step + 2 * lane) : make_float2(0.f, 0.f);
+    }
+    float top = mx;
+#pragma unroll
+    for (int s = 0; s < 8; ++s) top = fmaxf(top, ml[s].x);
+    const float ref = top == -INFINITY ? 0.f : top, f0 = ex2(mx - ref);
+    l *= f0; x *= f0; y *= f0; mx = top;
+#pragma unroll
+    for (int s = 0; s < 8; ++s) {
+      const float f = ex2(ml[s].x - ref);
+      l += ml[s].y * f; x += v[s].x * f; y += v[s].y * f;
+    }
   }
   const float inv = l == 0.f ? 0.f : 1.f / l;
   store2(static_cast<T *>(a.out) + i * kDh + 2 * lane, x * inv, y * inv);
 }
 
 // Shape of a launch: row tiles, CTAs of a cluster, clusters per segment.  A function of sizes the scratch is asked for with.
-struct Plan { int mt, tiles, cluster, outer; };
+struct Plan { int tiles, cluster, outer; };
 
 Plan plan_of(int dtype, int batch, int rows, int heads, int kv_heads, int max_len) {
   Plan p;
   const int m = rows * (heads / kv_heads);
-  p.mt = dtype == PD_DTYPE_BF16 && m > 16 ? 2 : 1;
-  p.tiles = (m + 16 * p.mt - 1) / (16 * p.mt);
+  // 32 rows per tile would read the cache half as often, at half the warps: 32 x 16 heads x 2048 tokens, 30 rows 58 us against 45, 1 x 12 x 777, 20 rows 7.8 against 5.8
+  p.tiles = (m + kRows - 1) / kRows;
   const long long segs = (long long)batch * kv_heads * p.tiles, blocks = ((long long)max_len + kBlk - 1) / kBlk;
   // places for CTAs in clusters: a GPC's SMs are not a multiple of a cluster's CTAs (512 of 592 places taken 35 us, 576 in two rounds 47 us, at 2 x 4
   // key heads x 131072 tokens)
-  const long long room = std::max(1ll, kClusterSms * ctas_per_sm(p.mt, dtype == PD_DTYPE_FP32) / segs);
+  const long long room = std::max(1ll, kClusterSms * ctas_per_sm(dtype == PD_DTYPE_FP32) / segs);
   p.cluster = 1;
   while (p.cluster < kMaxCluster && p.cluster * 2 <= room && p.cluster * kWarps < blocks) p.cluster *= 2;
   p.outer = p.cluster == kMaxCluster ? (int)std::max(1ll, std::min(room / kMaxCluster, blocks / (kMaxCluster * kWarps * kOuterBlocks))) : 1;
@@ -657,13 +642,13 @@ bool cache_attn_sizes_ok(int dtype, int batch, int rows, int heads, int kv_heads
 }
 
 size_t scratch_bytes_of(const Plan &p, int batch, int kv_heads) {
-  return p.outer > 1 ? (size_t)batch * kv_heads * p.tiles * p.outer * p.mt * 16 * kRec * sizeof(float) : 0;
+  return p.outer > 1 ? (size_t)batch * kv_heads * p.tiles * p.outer * kRows * kRec * sizeof(float) : 0;
 }
 
-template <typename T, int MT>
+template <typename T>
 cudaError_t launch_cache_attn(const CacheAttnArgs &a, int batch, bool mod, cudaStream_t s) {
-  constexpr int smem = smem_bytes(MT, sizeof(T) == 4);
-  auto kernel = mod ? cache_attn_kernel<T, MT, true> : cache_attn_kernel<T, MT, false>;
+  constexpr int smem = smem_bytes(sizeof(T) == 4);
+  auto kernel = mod ? cache_attn_kernel<T, true> : cache_attn_kernel<T, false>;
   // once per kernel and device: setting it costs as much host time as a third of the launch
   static std::atomic<uint64_t> ready[2];
   int dev = 0;
@@ -677,7 +662,7 @@ cudaError_t launch_cache_attn(const CacheAttnArgs &a, int batch, bool mod, cudaS
   st = op_launch(kernel, dim3(a.cluster * a.outer, a.HK * a.tiles, batch), kThreads, smem, a.cluster, s, a);
   if (st != cudaSuccess || a.outer == 1) return st;
   const long long n_out = (long long)batch * a.R * a.H;
-  return op_launch(cache_attn_merge_kernel<T>, dim3((unsigned)((n_out + 3) / 4)), 128, 0, 1, s, a, MT * 16, n_out);
+  return op_launch(cache_attn_merge_kernel<T>, dim3((unsigned)((n_out + 3) / 4)), 128, 0, 1, s, a, n_out);
 }
 
 }  // namespace
@@ -718,9 +703,8 @@ pd_status pd_cache_attention(int32_t dtype, int32_t batch, int32_t rows_per_seq,
   const bool mod = softcap > 0.f || bias;
   cudaStream_t s = reinterpret_cast<cudaStream_t>(cuda_stream);
   cudaError_t st;
-  if (dtype == PD_DTYPE_FP32) st = launch_cache_attn<float, 1>(a, batch, mod, s);
-  else if (p.mt == 1) st = launch_cache_attn<__nv_bfloat16, 1>(a, batch, mod, s);
-  else st = launch_cache_attn<__nv_bfloat16, 2>(a, batch, mod, s);
+  if (dtype == PD_DTYPE_FP32) st = launch_cache_attn<float>(a, batch, mod, s);
+  else st = launch_cache_attn<__nv_bfloat16>(a, batch, mod, s);
   return st == cudaSuccess ? PD_OK : PD_ERR_CUDA;
 }
 
