@@ -319,6 +319,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(sizeof(T) == 4)) cache_a
 #pragma unroll
     for (int jh = 0; jh < 8; jh += 4) {
       uint32_t u[4][4];
+      float rest[4][4];                                                            // the second parts' sums: the tensor cores drop what lies below a sum's last place
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const int token = 16 * (g >> 1) + 4 * ((jh + j) >> 1) + 2 * (j & 1) + (g & 1);
@@ -333,10 +334,17 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(sizeof(T) == 4)) cache_a
           widen(u[j][k], b0, b1);
 #pragma unroll
           for (int p = 0; p < NP; ++p) {
-            if (k + p == 0) mma_f16_first(s[jh + j], qf[p][k], b0, b1);
-            else mma_f16(s[jh + j], qf[p][k], b0, b1);
+            float (&c)[4] = p ? rest[j] : s[jh + j];
+            if (k == 0) mma_f16_first(c, qf[p][k], b0, b1);
+            else mma_f16(c, qf[p][k], b0, b1);
           }
         }
+      if (NP == 2) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+          for (int x = 0; x < 4; ++x) s[jh + j][x] += rest[j][x];
+      }
     }
     refill(i, 2 * i);
     // ---- the block's softmax; without cap and bias the scale (positive) comes in with the exponent
@@ -426,7 +434,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(sizeof(T) == 4)) cache_a
 #pragma unroll
       for (int dh = 0; dh < 8; dh += 4) {
         uint32_t u[4][4];
-        float tv[4][4];
+        float tv[4][4], rest[4][4];
 #pragma unroll
         for (int dn = 0; dn < 4; ++dn) {
           const uint4 w = lds128(vbase + ((dh + dn) * 8 + g) * kBlk + t * 16);
@@ -453,10 +461,17 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(sizeof(T) == 4)) cache_a
             widen(u[dn][k], b0, b1);
 #pragma unroll
             for (int p = 0; p < NP; ++p) {
-              if (k + p == 0) mma_f16_first(tv[dn], pf[p][k], b0, b1);
-              else mma_f16(tv[dn], pf[p][k], b0, b1);
+              float (&c)[4] = p ? rest[dn] : tv[dn];
+              if (k == 0) mma_f16_first(c, pf[p][k], b0, b1);
+              else mma_f16(c, pf[p][k], b0, b1);
             }
           }
+        if (NP == 2) {
+#pragma unroll
+          for (int dn = 0; dn < 4; ++dn)
+#pragma unroll
+            for (int x = 0; x < 4; ++x) tv[dn][x] += rest[dn][x];
+        }
 #pragma unroll
         for (int dn = 0; dn < 4; ++dn)
 #pragma unroll
