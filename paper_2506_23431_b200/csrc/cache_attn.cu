@@ -264,7 +264,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(sizeof(T) == 4)) cache_a
 #pragma unroll
     for (int k = 0; k < 16; ++k) mx = fmaxf(mx, fabsf(f[k]));
     mx = quad_max(mx);
-    const int e = min(max((int)(__float_as_uint(mx) >> 23) - 127, -100), 100);
+    const int e = min(max((int)(__float_as_uint(mx) >> 23) - 127, -126), 126);
     const float down = __uint_as_float((uint32_t)(127 - e) << 23);
     w.mul = __uint_as_float((uint32_t)(127 + e) << 23) * (MOD && a.cap_log2e > 0.f ? a.inv_cap : a.scale_log2e);
 #pragma unroll

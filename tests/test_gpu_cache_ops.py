@@ -332,7 +332,7 @@ def test_attention_against_plain_form(dtype, heads, kv, rows, lens, spans, n_bia
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
-@pytest.mark.parametrize("size", [1e-30, 1e-6, 1e4, 1e20])
+@pytest.mark.parametrize("size", [1e-37, 1e-30, 1e-6, 1e4, 1e20, 1e37])
 def test_attention_over_blocks_of_any_size(dtype, size):
     """Keys and queries of any magnitude (the product in range), blocks of values 2^40 apart: what a block of small weights and large values adds is not lost."""
     import torch
@@ -407,6 +407,81 @@ def test_attention_bad_blocks_and_counts():
     assert not _attend(c2, q2, [5], [-4], None, None, 0.0).any()
     assert not _attend(c2, q2, [0], [256], None, None, 0.0).any()
     _check(_attend(c2, q2, [5], [256], None, None, 0.0, max_len=100), R.attend(_host(q2), c2.codes, c2.scales, c2.table, [5], [100], 0.125), "bf16")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_bias_of_the_lowest_value_removes_positions(dtype):
+    """The type's lowest value, or minus infinity, as a mask by distance: the positions weigh nothing, a row with no others is zero."""
+    import torch
+    lens = [200]
+    c = _filled(37, lens, 2)
+    q = _dev(np.random.default_rng(4).standard_normal((1, 3, 128)), _dt(dtype))
+    for low in (-math.inf, float(np.finfo(np.float32).min)):
+        bias = np.zeros((2, 100), np.float32)
+        bias[0, 70:] = low                                        # head 0 sees the last 70 positions only, head 1 all
+        got = _attend(c, q, [3], lens, None, bias, 0.0)
+        near = R.attend(_host(q), c.codes, c.scales, c.table, [3], lens, 0.125, np.array([[[130, 200]] * 3]))
+        every = R.attend(_host(q), c.codes, c.scales, c.table, [3], lens, 0.125)
+        for h, want in ((0, near), (1, every)):
+            _check(got[..., h * 64:h * 64 + 64], tuple(w[..., h * 64:h * 64 + 64] for w in want), dtype)
+        bias[0] = low
+        assert not _attend(c, q, [3], lens, None, bias, 0.0)[..., :64].any()
+
+
+def test_operators_after_copies_and_joined_streams_in_a_graph():
+    """Each operator as the first node behind copies, a fill, and a join of two captured streams: it waits for all of them."""
+    import torch
+    from paper_2506_23431_b200 import binding as B
+    g = np.random.default_rng(41)
+    heads, n = 4, 3000
+    c = Cache(41, 1, 60, heads)
+    src = _dev(g.standard_normal((n, 3 * heads, 64)), torch.bfloat16)
+    x, kv, q, out = torch.empty_like(src), torch.empty_like(src), torch.empty(1, 8, heads * 64, dtype=torch.bfloat16, device="cuda"), torch.empty(1, 8, heads * 64, dtype=torch.bfloat16, device="cuda")
+    pos, turns = torch.zeros(n, dtype=torch.int32, device="cuda"), _dev(B.rotary_turns(64)[0])
+    want_pos = torch.arange(n, dtype=torch.int32, device="cuda")
+    zero, cnt, lens, rows = _i32([0]), _i32([n]), _i32([0]), _i32([8])
+    le = _i32([n])
+    scratch = torch.empty(B.cache_attention_scratch_bytes(1, 1, 8, heads, heads, 60 * 64), dtype=torch.uint8, device="cuda")
+
+    def chain(fork):
+        s, s2 = torch.cuda.current_stream(), torch.cuda.Stream()
+        if fork:
+            s2.wait_stream(s)
+            with torch.cuda.stream(s2):
+                kv.copy_(src)
+                lens.copy_(le)
+        else:
+            kv.copy_(src)
+            lens.copy_(le)
+        x.copy_(src)
+        pos.copy_(want_pos)
+        B.rotary(x, pos, turns, out=x)
+        if fork:
+            s.wait_stream(s2)
+        B.cache_append(kv[:, heads:2 * heads], kv[:, 2 * heads:], zero, cnt, zero, c.d_table, c.d_codes, c.d_scales, n)
+        q.zero_()
+        q.copy_(x[-8:, :heads].reshape(1, 8, heads * 64))
+        B.cache_attention(q, c.d_codes, c.d_scales, c.d_table, rows, lens, 0.125, out=out, scratch=scratch)
+
+    chain(False)
+    torch.cuda.synchronize()
+    want, codes = out.clone(), c.d_codes.clone()
+    s, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    with torch.cuda.stream(s):
+        chain(True)
+        torch.cuda.synchronize()
+        with torch.cuda.graph(graph, stream=s):
+            chain(True)
+    for _ in range(4):
+        for t in (x, kv, q, out, pos, lens):
+            t.zero_()
+        c.d_codes[c.d_table.long()[0, :47]] = 0x7F
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.isfinite(out).all() and torch.equal(out, want)
+        at = c.d_table.long()[0, :46]
+        assert torch.equal(c.d_codes[at], codes[at])
 
 
 def test_attention_strided_queries_and_batch_independence():
