@@ -35,12 +35,13 @@ struct AppendArgs {
   uint8_t *codes; float *scales; int32_t *status;
 };
 
-__device__ __forceinline__ uint32_t e4m3x2(float lo, float hi) {        // round to nearest even, saturating; NaN stays NaN
-  unsigned short r;
-  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+// Four codes in a word: round to nearest even, saturating; NaN stays NaN.
+__device__ __forceinline__ uint32_t e4m3x4(float a, float b, float c, float d) {
+  uint32_t r;
+  asm("{\n\t.reg .b16 lo, hi;\n\tcvt.rn.satfinite.e4m3x2.f32 lo, %2, %1;\n\tcvt.rn.satfinite.e4m3x2.f32 hi, %4, %3;\n\tmov.b32 %0, {lo, hi};\n\t}"
+      : "=r"(r) : "f"(a), "f"(b), "f"(c), "f"(d));
   return r;
 }
-__device__ __forceinline__ uint32_t e4m3x4(float a, float b, float c, float d) { return e4m3x2(a, b) | e4m3x2(c, d) << 16; }
 
 // The codes of four tokens (or dims) at another scale: times f, rounded again.
 __device__ __forceinline__ uint32_t rescale4(uint32_t w, float f) {
@@ -74,6 +75,26 @@ __device__ __forceinline__ void unpack8(const Raw8<__nv_bfloat16> &r, float (&f)
     f[2 * i] = __uint_as_float(u[i] << 16);
     f[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
   }
+}
+
+// Eight dims times a power of two, exact (bf16: two at a time; what gets too small for bf16 is far below the smallest code).
+__device__ __forceinline__ void scaled8(const Raw8<float> &r, float inv, float (&f)[8]) {
+  unpack8(r, f);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) f[i] *= inv;
+}
+__device__ __forceinline__ void scaled8(const Raw8<__nv_bfloat16> &r, float inv, float (&f)[8]) {
+  const __nv_bfloat162 by = __float2bfloat162_rn(inv);
+  const uint32_t u[4] = {r.v[0].x, r.v[0].y, r.v[0].z, r.v[0].w};
+  Raw8<__nv_bfloat16> s;
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const __nv_bfloat162 x = __hmul2(*reinterpret_cast<const __nv_bfloat162 *>(&u[i]), by);
+    w[i] = *reinterpret_cast<const uint32_t *>(&x);
+  }
+  s.v[0] = make_uint4(w[0], w[1], w[2], w[3]);
+  unpack8(s, f);
 }
 
 // Largest magnitude so far, by its bits, NaN left out: two at a time in bf16.
@@ -201,11 +222,7 @@ __global__ void __launch_bounds__(128, sizeof(T) == 2 ? 7 : 4) cache_append_kern
       if (tg[w] * 4 + 4 <= lo || tg[w] * 4 >= hi) continue;
       float f[4][8];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        unpack8(raw[w][k], f[k]);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) f[k][i] *= inv;
-      }
+      for (int k = 0; k < 4; ++k) scaled8(raw[w][k], inv, f[k]);
       if (w == 0) {
         uint8_t *p = dst + tg[w] * 4 * kDh + dg[w] * 8;
 #pragma unroll
