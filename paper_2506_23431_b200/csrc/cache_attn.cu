@@ -4,17 +4,22 @@
 //   score(row, p) = scale * q . k_p;  with a cap: cap * tanh(score / cap);  with a bias: + bias[head][min(end - 1 - p, n_bias - 1)]
 //   out(row) = softmax over the visible p (begin <= p < end, p < len) of score . v;  zero where nothing is visible
 //
-// Bound by the cache's bytes: 128 per (token, kv head), read once for all rows that share the head.  A segment is a
-// (sequence, kv head, tile of 16 rows; a row is a (query row, head of the group)); its blocks are split over CTAs, and in a CTA
-// over four warps that work alone: each streams its blocks - keys and values of a (block, head) are 8 KB in one piece -
-// through a ring of its own with bulk copies, and reads them with 16-byte loads straight in the order the tensor cores take them, because a contraction does not
-// see the order of its terms:
+// Bound by the cache's bytes: 128 per (token, kv head), read once for the rows of a tile.  A segment is a (sequence, kv head, tile of 16 rows; a row is a
+// (query row, head of the group)); its blocks are split over the CTAs of a cluster and, where segments are few and long, over several clusters, and in a CTA
+// over four warps that work alone: each streams its blocks - keys and values of a (block, head) are 4 KB each, in one
+// piece - through a ring of its own with bulk copies, and reads them with 16-byte loads straight in the order the tensor
+// cores take them, because a contraction does not see the order of its terms:
 //   keys    [token][dim]: lane (g, t) takes dims 16 t .. 16 t + 15 of a token, four for each of four k16 steps; the queries have the same order;
 //   values  [dim][token]: lane (g, t) takes tokens 16 t .. 16 t + 15 of a dim; column c of score tile j is therefore token
 //           16 (c >> 1) + 4 (j >> 1) + 2 (j & 1) + (c & 1), and the scores are the next product's operand where they stand.
 // Codes are widened to f16 pairs (exact).  Every block has its own maximum: weights 2^(s - max + 15) keep 11 bits down to 2^-29 of
 // the largest in f16, the block's sum of values is a fresh accumulator, and only then do the running maximum and the values' scale come in, in 32 bits - a
-// block of tiny weights and large values loses nothing.  32-bit queries and weights go through two f16 parts (22 bits).
+// block of tiny weights and large values loses nothing.  32-bit queries and weights go through two f16 parts (22 bits), each with its own sums.
+//
+// Sixteen warps per SM with four independent products each: with eight warps and products in chains a launch of 32 sequences x 16 heads x 2048 tokens, 12
+// rows, took 56 us, now 28.4 (134 MB, 4.8 TB/s; every further 2048 tokens 21.3 us, 6.3 TB/s: what is left is the launch, one round of loads, and the last
+// blocks' work and join).  Loads alone take 25.  1 x 12 heads x 777 tokens 5.6 us, 2 x 4 key heads x 131072 tokens 31.2, of which 2.3 the merge of eight clusters.
+// A cap costs 2 us in 13, a bias over the table's distances as much.
 #include <cuda_fp16.h>
 #include <float.h>
 #include <limits.h>
@@ -35,8 +40,8 @@ constexpr int kWarps = 4, kThreads = kWarps * 32;
 constexpr int kMaxCluster = 8, kClusterSms = 128;
 constexpr int kOuterBlocks = 4;                   // fewest blocks for each warp where a segment is split beyond a cluster
 constexpr int kRows = 16;                         // rows of a tile
-// CTAs per SM as the registers allow (128 a thread; two f16 parts 168), and slots of 4 KB (a block's keys, or its values) in a warp's ring: what then fits the
-// shared memory.
+// CTAs per SM as the registers allow (128 a thread; two f16 parts 168), and slots of 4 KB (a block's keys, or its values) in a warp's ring: what then
+// fits the shared memory (a fifth of a kilobyte more per CTA and one fewer is resident: 28 -> 37 us).
 __host__ __device__ constexpr int ctas_per_sm(bool f32) { return f32 ? 3 : 4; }
 __host__ __device__ constexpr int slots(bool f32) { return f32 ? 4 : 3; }
 constexpr int kRec = kDh + 4;                     // a row's partial result: 64 sums, maximum, sum of weights, alignment
