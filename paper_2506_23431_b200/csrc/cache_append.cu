@@ -8,10 +8,14 @@
 //
 // A scale that is a power of two costs a format with an exponent of its own nothing but part of its subnormal range, and makes every division
 // exact: the codes do not depend on the precision they are computed in, and a block whose scale grows keeps its older
-// codes bit for bit, but for those that leave the normal range.
+// tokens' values as they are, but for those that leave the normal range.
 //
-// One CTA per (head, keys | values), walking a sequence's blocks.  A thread holds four tokens of eight dims, so that it
+// One CTA per head, walking a sequence's blocks.  A thread holds four tokens of eight dims, of the keys and of the values, so that it
 // writes keys as 8 bytes per token and values, whose layout is turned, as whole words of four tokens, with no pass through shared memory.
+// Reads every element once (2 or 4 bytes) and writes a byte: 32 x 16 heads x 2048 bf16 tokens 64.4 us, 6.2 TB/s, 95 % of the copy rate; sequences
+// of 0 to 2048 tokens 38.6 us (82 %: the longest ones' CTAs end last); one token for each of 64 sequences 4.6 us, a chain of
+// counts, table, scale and store.  It took eight 16-byte loads under way per thread and packed arithmetic: with four, and
+// element by element, instruction issue bound it (55 us where the bytes take 31.6).
 #include <cuda_fp16.h>
 
 #include <algorithm>
@@ -25,7 +29,7 @@ namespace {
 
 constexpr int kBlk = PD_CACHE_BLOCK;
 constexpr int kPart = kBlk * kDh;                 // codes of a block's keys (values) of one head
-constexpr long long kAppendCtas = 64 * kSms;
+constexpr long long kAppendCtas = 64 * kSms;      // about nine waves: with 24 per SM the ends of unequal sequences cost 5 %, with 400 the starts of CTAs
 
 struct AppendArgs {
   int heads, n_blocks, max_blocks, rows, max_new;
