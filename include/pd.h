@@ -488,8 +488,8 @@ PD_API pd_status pd_cache_append(int32_t dtype, int32_t batch, int32_t n_kv_head
  *              needs no clearing, holds nothing between calls; calls that may overlap on the GPU need one each
  *   status     device int32 or NULL: set to PD_ERR_ARG for a block outside 0 .. n_blocks among those that are read (its positions
  *              count as not there), to PD_ERR_TIMEOUT if a bounded wait inside the kernel expired; otherwise left alone
- * Codes behind a sequence's last token, and those that a row does not see, never matter, numbers or not.  Results do not depend on the other
- * sequences of the batch, and repeat bit for bit.  Enqueues on cuda_stream and returns; allocates nothing on the device.
+ * Codes behind a sequence's last token, and those that a row does not see, never matter, numbers or not.  Results repeat bit for bit; what the
+ * other sequences of the batch hold does not change them (the sizes of the call set the order of the sums).  Enqueues on cuda_stream and returns; allocates nothing on the device.
  * PD_ERR_ARG for null pointers, misaligned buffers or sizes out of range, PD_ERR_WORKSPACE for a scratch that is
  * too small, PD_ERR_CUDA if a launch fails. */
 PD_API size_t pd_cache_attention_scratch_bytes(int32_t dtype, int32_t batch, int32_t rows_per_seq, int32_t n_heads, int32_t n_kv_heads,

@@ -264,8 +264,7 @@ extern "C" pd_status pd_cache_append(int32_t dtype, int32_t batch, int32_t n_kv_
   if (!k || !v || !row_start || !n_new || !pos_start || !table || !codes || !scales) return PD_ERR_ARG;
   const int e = dtype == PD_DTYPE_BF16 ? 2 : 4;
   if (k_stride < (int64_t)n_kv_heads * kDh || v_stride < (int64_t)n_kv_heads * kDh || (k_stride * e) % 16 != 0 || (v_stride * e) % 16 != 0) return PD_ERR_ARG;
-  if ((reinterpret_cast<uintptr_t>(k) | reinterpret_cast<uintptr_t>(v) | reinterpret_cast<uintptr_t>(codes)) % 16 != 0 ||
-      reinterpret_cast<uintptr_t>(scales) % 8 != 0) return PD_ERR_ARG;
+  if (!aligned_to(16, k, v, codes) || !aligned_to(8, scales) || !aligned_to(4, row_start, n_new, pos_start, table, status)) return PD_ERR_ARG;
   AppendArgs a;
   a.heads = n_kv_heads; a.n_blocks = n_blocks; a.max_blocks = max_blocks; a.rows = rows; a.max_new = max_new;
   a.k = k; a.v = v; a.k_stride = k_stride; a.v_stride = v_stride;

@@ -704,8 +704,7 @@ pd_status pd_cache_attention(int32_t dtype, int32_t batch, int32_t rows_per_seq,
   if (!(attn_scale > 0.f) || !(attn_scale < 1e30f) || !(softcap >= 0.f) || !(softcap < 1e30f) || (bias && (n_bias < 1 || n_bias > (1 << 20)))) return PD_ERR_ARG;
   const int e = dtype == PD_DTYPE_BF16 ? 2 : 4;
   if (q_stride < (int64_t)n_heads * kDh || (q_stride * e) % 16 != 0) return PD_ERR_ARG;
-  if ((reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(codes) | reinterpret_cast<uintptr_t>(out)) % 16 != 0 ||
-      (reinterpret_cast<uintptr_t>(scales) | reinterpret_cast<uintptr_t>(spans)) % 8 != 0 || reinterpret_cast<uintptr_t>(scratch) % 16 != 0) return PD_ERR_ARG;
+  if (!aligned_to(16, q, codes, out, scratch) || !aligned_to(8, scales, spans) || !aligned_to(4, table, n_rows, lens, bias, status)) return PD_ERR_ARG;
   const Plan p = plan_of(dtype, batch, rows_per_seq, n_heads, n_kv_heads, max_len);
   if ((long long)n_kv_heads * p.tiles > 65535) return PD_ERR_ARG;
   const size_t need = scratch_bytes_of(p, batch, n_kv_heads);

@@ -2,8 +2,13 @@
 #pragma once
 
 #include <cuda_runtime.h>
+#include <stdint.h>
 
 namespace pd {
+
+// Whether every address (null ones among them) is a multiple of n.
+template <typename... P>
+bool aligned_to(uintptr_t n, P... p) { return ((reinterpret_cast<uintptr_t>(p) | ...) % n) == 0; }
 
 // Everything enqueued before is complete and visible behind this; the kernel's first instruction.  What follows it in the stream may then be brought
 // onto the SMs while the kernel runs, up to its own wait: 1 to 2 us per launch between two of these operators.

@@ -279,8 +279,7 @@ pd_status pd_rotary(int32_t dtype, int32_t tokens, int32_t n_heads, int32_t d_he
   if (tokens == 0) return PD_OK;
   if (!x || !positions || !turns || !out) return PD_ERR_ARG;
   const size_t e = dtype == PD_DTYPE_BF16 ? 2 : 4;
-  if ((reinterpret_cast<uintptr_t>(x) | reinterpret_cast<uintptr_t>(out)) % e != 0 || reinterpret_cast<uintptr_t>(positions) % 4 != 0 ||
-      reinterpret_cast<uintptr_t>(turns) % 8 != 0) return PD_ERR_ARG;
+  if (!aligned_to(e, x, out) || !aligned_to(4, positions) || !aligned_to(8, turns)) return PD_ERR_ARG;
   // the output's heads must not overlap: heads inside tokens, or tokens inside heads
   const bool by_token = (n_heads == 1 || out_head_stride >= d_head) && (tokens == 1 || out_token_stride >= (n_heads - 1) * out_head_stride + d_head);
   const bool by_head = (tokens == 1 || out_token_stride >= d_head) && (n_heads == 1 || out_head_stride >= (tokens - 1) * out_token_stride + d_head);
@@ -296,7 +295,7 @@ pd_status pd_rotary(int32_t dtype, int32_t tokens, int32_t n_heads, int32_t d_he
   // as many tokens per CTA as leave four CTAs per SM
   a.tok_per_cta = max(1, min(kRotMaxTokens, tokens / (4 * kSms)));
   const int vec = (int)(16 / e);
-  const bool pieces = (reinterpret_cast<uintptr_t>(x) | reinterpret_cast<uintptr_t>(out)) % 16 == 0 &&
+  const bool pieces = aligned_to(16, x, out) &&
                       (x_token_stride | x_head_stride | out_token_stride | out_head_stride) % vec == 0 && d_head % vec == 0;
   const bool wide = pieces && (interleaved ? rot_dim : rot_dim / 2) % vec == 0;
   cudaStream_t s = reinterpret_cast<cudaStream_t>(cuda_stream);

@@ -96,7 +96,7 @@ def test_nothing_to_do_is_no_error():
 
 @pytest.mark.parametrize("bad", [dict(dtype=-1), dict(batch=0), dict(batch=65536), dict(heads=0), dict(n_blocks=0), dict(max_blocks=0), dict(rows=-1), dict(max_new=-1), dict(k=None),
                                  dict(v=None), dict(table=None), dict(codes=None), dict(scales=None), dict(n_new=None), dict(pos=None), dict(row_start=None), dict(k=P + 8), dict(codes=P + 4),
-                                 dict(ks=128), dict(vs=196), dict(scales=P + 4)])
+                                 dict(ks=128), dict(vs=196), dict(scales=P + 4), dict(table=P + 2), dict(n_new=P + 1), dict(row_start=P + 2), dict(pos=P + 2), dict(status=P + 2)])
 def test_append_refuses(bad):
     assert _call("pd_cache_append", APPEND, **bad) == -1
 
@@ -104,7 +104,7 @@ def test_append_refuses(bad):
 @pytest.mark.parametrize("bad", [dict(dtype=3), dict(batch=0), dict(rows=0), dict(rows=65), dict(heads=7), dict(heads=2), dict(kv=0), dict(n_blocks=0), dict(max_blocks=0), dict(max_len=-1),
                                  dict(scale=0.0), dict(scale=math.nan), dict(scale=math.inf), dict(cap=-1.0), dict(cap=math.nan), dict(q=None), dict(codes=None), dict(table=None),
                                  dict(n_rows=None), dict(lens=None), dict(out=None), dict(q=P + 8), dict(out=P + 8), dict(qs=320), dict(qs=388), dict(spans=P + 4), dict(bias=P, n_bias=0),
-                                 dict(scales=P + 4), dict(scratch=P + 8)])
+                                 dict(scales=P + 4), dict(scratch=P + 8), dict(table=P + 2), dict(lens=P + 2), dict(n_rows=P + 1), dict(bias=P + 2, n_bias=4), dict(status=P + 2)])
 def test_attention_refuses(bad):
     assert _call("pd_cache_attention", ATTEND, **bad) == -1
 

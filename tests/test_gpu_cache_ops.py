@@ -606,6 +606,40 @@ def test_captured_steps_follow_their_tensors():
         assert torch.isfinite(out).all() and torch.equal(out, want) and torch.equal(c.d_scales[c.d_table.long()[:, p // 64]], e.d_scales[e.d_table.long()[:, p // 64]])
 
 
+def test_sequences_that_share_blocks_and_many_short_ones():
+    """A prefix held once for several sequences; a batch far larger than the GPU has places for, lengths from none."""
+    import torch
+    from paper_2506_23431_b200 import binding as B
+    c = _filled(43, [200], 2)
+    table = np.repeat(c.table, 3, axis=0)
+    q = _dev(np.random.default_rng(6).standard_normal((3, 2, 256)), torch.bfloat16)
+    lens = [200, 130, 64]
+    out = B.cache_attention(q, c.d_codes, c.d_scales, _i32(table), _i32([2, 2, 2]), _i32(lens), 0.125)
+    _check(out, R.attend(_host(q), c.codes, c.scales, table, [2, 2, 2], lens, 0.125), "bf16")
+    n = 3000
+    table = np.repeat(c.table, n, axis=0)
+    lens = np.arange(n) % 201
+    q = _dev(np.random.default_rng(7).standard_normal((n, 1, 128)), torch.bfloat16)
+    out = B.cache_attention(q, c.d_codes, c.d_scales, _i32(table), _i32(np.ones(n)), _i32(lens), 0.125)
+    some = list(range(0, n, 97))
+    _check(out[some], R.attend(_host(q[some]), c.codes, c.scales, table[some], [1] * len(some), lens[some], 0.125), "bf16")
+
+
+def test_no_tokens():
+    import torch
+    from paper_2506_23431_b200 import binding as B
+    x = torch.zeros(0, 3, 64, dtype=torch.bfloat16, device="cuda")
+    assert B.rotary(x, _i32(np.zeros(0)), _dev(B.rotary_turns(64)[0])).shape == (0, 3, 64)
+    c = _filled(47, [70], 2)
+    before = c.d_codes.clone()
+    k = torch.zeros(0, 2, 64, dtype=torch.bfloat16, device="cuda")
+    B.cache_append(k, k, _i32([0]), _i32([0]), _i32([70]), c.d_table, c.d_codes, c.d_scales, 0)
+    B.cache_append(torch.ones(5, 2, 64, device="cuda"), torch.ones(5, 2, 64, device="cuda"), _i32([0]), _i32([0]), _i32([70]), c.d_table, c.d_codes, c.d_scales, 5)
+    assert torch.equal(c.d_codes, before)
+    out = B.cache_attention(torch.ones(1, 2, 128, dtype=torch.bfloat16, device="cuda"), c.d_codes, c.d_scales, c.d_table, _i32([2]), _i32([0]), 0.125, 0)
+    assert not out.any()
+
+
 def test_calls_on_two_streams_at_once():
     import torch
     lens = [5000]
