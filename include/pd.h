@@ -420,8 +420,8 @@ PD_API const char *pd_static_last_error(void);
  *   sizes       tokens >= 0; d_head 2..256; rot_dim even, 2..d_head
  *   x, out      device; element (token, head, dim) at token * token_stride + head * head_stride + dim (strides in elements, not
  *               negative; x may repeat, heads of out must not overlap).  Slices of a fused projection's rows will do.  out may be x
- *               with the same strides, else they must not overlap.  Addresses and strides that are multiples of 16 bytes,
- *               with rot_dim / 2 (interleaved: rot_dim) and d_head multiples of 16 bytes too, take the fast path
+ *               with the same strides, else they must not overlap.  Fastest with addresses, strides and d_head that
+ *               are multiples of 16 bytes, and rot_dim / 2 (interleaved: rot_dim) likewise; any alignment to an element will do
  *   positions   device int32 [tokens], any sign;  turns  device double [rot_dim / 2]: turns per position of every pair
  * pd_rotary_turns fills turns (host [rot_dim / 2]) and *amplitude (host or NULL): theta^(-2 i / rot_dim) / 2 pi,
  *   PD_ROTARY_PLAIN     as it is

@@ -54,6 +54,22 @@ template <> struct Piece<__nv_bfloat16, 8> {
     v = make_uint4(u[0], u[1], u[2], u[3]);
   }
 };
+template <> struct Piece<float, 2> {
+  float2 v;
+  __device__ __forceinline__ void unpack(float (&f)[2]) const { f[0] = v.x; f[1] = v.y; }
+  __device__ __forceinline__ void pack(const float (&f)[2]) { v = make_float2(f[0], f[1]); }
+};
+template <> struct Piece<__nv_bfloat16, 4> {
+  uint2 v;
+  __device__ __forceinline__ void unpack(float (&f)[4]) const {
+    f[0] = __uint_as_float(v.x << 16); f[1] = __uint_as_float(v.x & 0xffff0000u);
+    f[2] = __uint_as_float(v.y << 16); f[3] = __uint_as_float(v.y & 0xffff0000u);
+  }
+  __device__ __forceinline__ void pack(const float (&f)[4]) {
+    const __nv_bfloat162 a = __floats2bfloat162_rn(f[0], f[1]), b = __floats2bfloat162_rn(f[2], f[3]);
+    v = make_uint2(*reinterpret_cast<const uint32_t *>(&a), *reinterpret_cast<const uint32_t *>(&b));
+  }
+};
 template <> struct Piece<float, 1> {
   float v;
   __device__ __forceinline__ void unpack(float (&f)[1]) const { f[0] = v; }
@@ -68,7 +84,7 @@ template <> struct Piece<__nv_bfloat16, 1> {
 // u c + v s, written out so that every form of the kernel gives the same bits.
 __device__ __forceinline__ float turned(float u, float c, float v, float s) { return fmaf(u, c, __fmul_rn(v, s)); }
 
-// VEC elements per access: 16 bytes, or 1 where the shape, the strides or the addresses do not allow it.  An item is what one thread
+// VEC elements per access: 16 bytes, 8 where the pairs or the strides allow no more, or 1 where they allow neither.  An item is what one thread
 // turns of a head at a time - VEC pairs (halves), VEC / 2 pairs (neighbours), one pair where VEC is 1 - or copies of its rest.  A thread
 // keeps its item (or one every 256) and takes it of several tokens at once: loads of kBatch tokens are under way together, the first ones
 // while sines and cosines are computed.
@@ -158,27 +174,29 @@ __global__ void __launch_bounds__(kRotThreads, 4) rotary_kernel(RotaryArgs a) {
 }
 
 // Heads whose rows are 16-byte pieces but whose pairs are not (half a rotated part that is no multiple of a piece, an odd number of pairs): whole head
-// rows pass through shared memory, so that loads and stores stay whole pieces and a dim finds its partner wherever it stands.
-// (65536 x 32 heads, 20 of 64 dims by halves: 150 us; element by element 452, which is left for what is not aligned.)
+// rows pass through shared memory, so that loads and stores stay whole pieces, and are turned there pair by pair.
+// (65536 x 32 heads, 20 of 64 dims by halves: 115 us; element by element 452, which is left for what is not aligned.)
 template <typename T, bool INTERLEAVED>
 __global__ void __launch_bounds__(kRotThreads, 4) rotary_staged_kernel(RotaryArgs a) {
   constexpr int VEC = 16 / sizeof(T);
   using V = Piece<T, VEC>;
   using E = Piece<T, 1>;
   __shared__ float2 cs[kRotMaxTokens * kRotMaxHead / 2];
-  __shared__ V stage[2][kBatch][kRotThreads];
+  __shared__ V stage[2][kBatch * kRotThreads];                          // head rows one after the other
   op_begin();
   const int half = a.rot / 2, tok0 = blockIdx.x * a.tok_per_cta, nt = min(a.tok_per_cta, a.tokens - tok0);
   const int chunks = a.dh / VEC, pass = kRotThreads / chunks, mine = threadIdx.x / chunks, c = threadIdx.x - mine * chunks, rows = nt * a.heads;
   V piece[kBatch];
-  auto row_of = [&](int r, int &tt, int &h) { tt = r / a.heads; h = r - tt * a.heads; };
+  // piece c of row r of the CTA, in x or out
+  auto at = [&](auto *base, long long tok, long long head, int r) {
+    const int tt = r / a.heads;
+    return base + (tok0 + tt) * tok + (r - tt * a.heads) * head + c * VEC;
+  };
   auto load = [&](int r0) {
 #pragma unroll
     for (int k = 0; k < kBatch; ++k) {
       const int r = r0 + k * pass + mine;
-      int tt, h;
-      row_of(r, tt, h);
-      if (mine < pass && r < rows) piece[k] = *reinterpret_cast<const V *>(static_cast<const T *>(a.x) + (tok0 + tt) * a.x_tok + h * a.x_head + c * VEC);
+      if (mine < pass && r < rows) piece[k] = *reinterpret_cast<const V *>(at(static_cast<const T *>(a.x), a.x_tok, a.x_head, r));
     }
   };
   load(0);
@@ -188,36 +206,31 @@ __global__ void __launch_bounds__(kRotThreads, 4) rotary_staged_kernel(RotaryArg
     sincospif((float)(2.0 * (t - rint(t))), &s, &co);
     cs[i] = make_float2(co * a.amplitude, (a.inverse ? -s : s) * a.amplitude);
   }
+  const int rows_step = kRotThreads / half, row0 = threadIdx.x / half, pair = threadIdx.x - row0 * half;      // a thread turns one pair of every rows_step-th row
   for (int r0 = 0, buf = 0; r0 < rows; r0 += kBatch * pass, buf ^= 1) {
+    if (mine < pass) {
 #pragma unroll
-    for (int k = 0; k < kBatch; ++k) stage[buf][k][threadIdx.x] = piece[k];
+      for (int k = 0; k < kBatch; ++k) stage[buf][k * pass * chunks + threadIdx.x] = piece[k];
+    }
     __syncthreads();                                                    // of the buffer before the last all reads are done, too
     load(r0 + kBatch * pass);
+    if (row0 < rows_step) {
+      for (int m = row0; m < min(kBatch * pass, rows - r0); m += rows_step) {
+        E *row = reinterpret_cast<E *>(&stage[buf][m * chunks]);
+        E &ea = row[INTERLEAVED ? 2 * pair : pair], &eb = row[INTERLEAVED ? 2 * pair + 1 : pair + half];
+        const float2 z = cs[(r0 + m) / a.heads * half + pair];
+        float xa[1], xb[1];
+        ea.unpack(xa); eb.unpack(xb);
+        const float ya[1] = {turned(xa[0], z.x, -xb[0], z.y)}, yb[1] = {turned(xb[0], z.x, xa[0], z.y)};
+        ea.pack(ya); eb.pack(yb);
+      }
+    }
+    __syncthreads();
     if (mine >= pass || (c * VEC >= a.rot && !a.copy_rest)) continue;
 #pragma unroll
     for (int k = 0; k < kBatch; ++k) {
       const int r = r0 + k * pass + mine;
-      if (r >= rows) break;
-      int tt, h;
-      row_of(r, tt, h);
-      V out = stage[buf][k][threadIdx.x];
-      if (c * VEC < a.rot) {
-        const E *row = reinterpret_cast<const E *>(&stage[buf][k][mine * chunks]);
-        float x[VEC];
-        out.unpack(x);
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-          const int d = c * VEC + e;
-          if (d >= a.rot) break;
-          const bool first = INTERLEAVED ? !(d & 1) : d < half;
-          const float2 z = cs[tt * half + (INTERLEAVED ? d >> 1 : first ? d : d - half)];
-          float y[1];
-          row[INTERLEAVED ? d ^ 1 : first ? d + half : d - half].unpack(y);
-          x[e] = turned(x[e], z.x, first ? -y[0] : y[0], z.y);
-        }
-        out.pack(x);
-      }
-      *reinterpret_cast<V *>(static_cast<T *>(a.out) + (tok0 + tt) * a.o_tok + h * a.o_head + c * VEC) = out;
+      if (r < rows) *reinterpret_cast<V *>(at(static_cast<T *>(a.out), a.o_tok, a.o_head, r)) = stage[buf][k * pass * chunks + threadIdx.x];
     }
   }
 }
@@ -232,8 +245,9 @@ template <typename T, int VEC>
 cudaError_t launch_rotary(const RotaryArgs &a, int interleaved, cudaStream_t s) {
   const int pairs = VEC == 1 ? 1 : interleaved ? VEC / 2 : VEC;
   const long long per_tok = ((long long)a.rot / 2 / pairs + (a.copy_rest ? (a.dh - a.rot) / VEC : 0)) * a.heads;
-  // whole groups of a token's items, so that few threads have none
-  const int threads = per_tok >= kRotThreads ? kRotThreads : (int)((kRotThreads / per_tok * per_tok + 31) / 32 * 32);
+  // whole groups of a token's items, or even shares of them, so that few threads have none
+  const long long shares = (per_tok + kRotThreads - 1) / kRotThreads, busy = shares > 1 ? (per_tok + shares - 1) / shares : kRotThreads / per_tok * per_tok;
+  const int threads = (int)((busy + 31) / 32 * 32);
   const int grid = (a.tokens + a.tok_per_cta - 1) / a.tok_per_cta;
   return op_launch(interleaved ? rotary_kernel<T, true, VEC> : rotary_kernel<T, false, VEC>, dim3(grid), threads, 0, 1, s, a);
 }
@@ -294,14 +308,22 @@ pd_status pd_rotary(int32_t dtype, int32_t tokens, int32_t n_heads, int32_t d_he
   a.copy_rest = !in_place && rot_dim < d_head;
   // as many tokens per CTA as leave four CTAs per SM
   a.tok_per_cta = max(1, min(kRotMaxTokens, tokens / (4 * kSms)));
-  const int vec = (int)(16 / e);
-  const bool pieces = aligned_to(16, x, out) &&
-                      (x_token_stride | x_head_stride | out_token_stride | out_head_stride) % vec == 0 && d_head % vec == 0;
-  const bool wide = pieces && (interleaved ? rot_dim : rot_dim / 2) % vec == 0;
+  // whether heads fall into pieces of so many bytes, and the pairs into whole pieces too
+  auto pieces = [&](int bytes) {
+    return aligned_to(bytes, x, out) && ((x_token_stride | x_head_stride | out_token_stride | out_head_stride) * (int64_t)e) % bytes == 0 && d_head * e % bytes == 0;
+  };
+  auto whole = [&](int bytes) { return pieces(bytes) && (interleaved ? rot_dim : rot_dim / 2) * e % bytes == 0; };
+  // pieces of 8 bytes cost the whole head, the way through shared memory the turned pairs (65536 x 32 bf16 heads by halves, 56 of 64 dims 134 us against 162; 32768 in
+  // fp32, 20 of 64 dims 170 against 115)
+  const bool by_eight = whole(8) && (rot_dim * 4 > d_head * 3 || !pieces(16));
   cudaStream_t s = reinterpret_cast<cudaStream_t>(cuda_stream);
   cudaError_t st;
-  if (dtype == PD_DTYPE_BF16) st = wide ? launch_rotary<__nv_bfloat16, 8>(a, interleaved, s) : pieces ? launch_rotary_staged<__nv_bfloat16>(a, interleaved, s) : launch_rotary<__nv_bfloat16, 1>(a, interleaved, s);
-  else st = wide ? launch_rotary<float, 4>(a, interleaved, s) : pieces ? launch_rotary_staged<float>(a, interleaved, s) : launch_rotary<float, 1>(a, interleaved, s);
+  if (dtype == PD_DTYPE_BF16)
+    st = whole(16) ? launch_rotary<__nv_bfloat16, 8>(a, interleaved, s) : by_eight ? launch_rotary<__nv_bfloat16, 4>(a, interleaved, s)
+       : pieces(16) ? launch_rotary_staged<__nv_bfloat16>(a, interleaved, s) : launch_rotary<__nv_bfloat16, 1>(a, interleaved, s);
+  else
+    st = whole(16) ? launch_rotary<float, 4>(a, interleaved, s) : by_eight ? launch_rotary<float, 2>(a, interleaved, s)
+       : pieces(16) ? launch_rotary_staged<float>(a, interleaved, s) : launch_rotary<float, 1>(a, interleaved, s);
   return st == cudaSuccess ? PD_OK : PD_ERR_CUDA;
 }
 

@@ -38,6 +38,7 @@ ROTARY = [
     ("bf16", 33, 5, 64, 48, False, True, 1 << 20), ("bf16", 33, 5, 64, 40, True, True, 4096), ("bf16", 9, 3, 64, 2, False, False, 4096), ("bf16", 9, 3, 64, 20, False, False, 4096),
     ("bf16", 17, 2, 128, 32, True, False, 1 << 22), ("bf16", 3, 2, 256, 256, False, False, 4096), ("bf16", 11, 3, 10, 6, True, False, 50),
     ("bf16", 4801, 24, 64, 20, False, False, 4096), ("fp32", 4801, 20, 64, 10, True, True, 4096), ("bf16", 700, 3, 64, 56, False, False, 4096), ("bf16", 6000, 5, 72, 18, True, False, 4096),
+    ("bf16", 900, 33, 64, 56, False, True, 4096), ("bf16", 40, 3, 68, 24, True, False, 4096), ("fp32", 700, 9, 64, 60, False, False, 4096), ("fp32", 50, 7, 62, 20, True, False, 4096),
     ("fp32", 1, 12, 64, 64, True, False, 100), ("fp32", 1201, 7, 64, 64, False, True, 1 << 30), ("fp32", 77, 5, 64, 40, True, False, 1 << 20), ("fp32", 13, 4, 80, 22, False, False, 4096),
 ]
 
