@@ -314,7 +314,7 @@ pd_status pd_rotary(int32_t dtype, int32_t tokens, int32_t n_heads, int32_t d_he
   };
   auto whole = [&](int bytes) { return pieces(bytes) && (interleaved ? rot_dim : rot_dim / 2) * e % bytes == 0; };
   // pieces of 8 bytes cost the whole head, the way through shared memory the turned pairs (65536 x 32 bf16 heads by halves, 56 of 64 dims 134 us against 162; 32768 in
-  // fp32, 20 of 64 dims 170 against 115)
+  // fp32, 20 of 64 dims 170 against 95)
   const bool by_eight = whole(8) && (rot_dim * 4 > d_head * 3 || !pieces(16));
   cudaStream_t s = reinterpret_cast<cudaStream_t>(cuda_stream);
   cudaError_t st;
