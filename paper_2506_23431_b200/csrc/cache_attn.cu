@@ -38,7 +38,9 @@ constexpr int kBlk = PD_CACHE_BLOCK;
 constexpr int kPart = kBlk * kDh;                 // codes of a block's keys (values) of one head
 constexpr int kWarps = 4, kThreads = kWarps * 32;
 constexpr int kMaxCluster = 8, kClusterSms = 128;
-constexpr int kOuterBlocks = 4;                   // fewest blocks for each warp where a segment is split beyond a cluster
+// Fewest blocks for each warp where a segment is split beyond a cluster: what a merge costs (12 heads x 16384 tokens 10.3 us, with four 12.7; 1 x 32768 8.6
+// and 11.1; 12 x 4096 would go from 6.8 to about 9 with one).
+constexpr int kOuterBlocks = 2;
 constexpr int kRows = 16;                         // rows of a tile
 // CTAs per SM as the registers allow (128 a thread; two f16 parts 168), and slots of 4 KB (a block's keys, or its values) in a warp's ring: what then
 // fits the shared memory (a fifth of a kilobyte more per CTA and one fewer is resident: 28 -> 37 us).
