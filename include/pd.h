@@ -486,6 +486,7 @@ PD_API pd_status pd_cache_append(int32_t dtype, int32_t batch, int32_t n_kv_head
  *              values below -2e38 count as minus infinity: such a position weighs nothing, and a row without others is zero
  *   scratch    device, 16-byte aligned, at least pd_cache_attention_scratch_bytes(...): partial results where a sequence is split;
  *              needs no clearing, holds nothing between calls; calls that may overlap on the GPU need one each
+ *              (256 bytes where no sequence is split: not touched then, and NULL with 0 bytes will do)
  *   status     device int32 or NULL: set to PD_ERR_ARG for a block outside 0 .. n_blocks among those that are read (its positions
  *              count as not there), to PD_ERR_TIMEOUT if a bounded wait inside the kernel expired; otherwise left alone
  * Codes behind a sequence's last token, and those that a row does not see, never matter, numbers or not.  Results repeat bit for bit; what the
