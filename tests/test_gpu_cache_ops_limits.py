@@ -1,0 +1,61 @@
+"""The operators around the 8-bit paged cache at the ends of what their documentation allows: caps, biases, scores and values of any
+size, bad blocks between good ones, walks of many blocks, counts of zero, launches that fail."""
+import math
+
+import numpy as np
+import pytest
+
+from tests import cache_reference as R
+from tests.test_gpu_cache_ops import _dev, _host, _i32
+
+pytestmark = pytest.mark.gpu
+
+
+# ---- append ----------------------------------------------------------------------------------------------------
+def _same_rows_everywhere(batch, heads, n, bad, seed, plant=None):
+    """Sequences that all receive the same rows, for more (sequence, head) pairs than one CTA each per block; blocks j of a sequence with
+    bad(j) have no valid id.  Compares every sequence with the plain form of one; returns the status word."""
+    import torch
+    from paper_2506_23431_b200 import binding as B
+    g = np.random.default_rng(seed)
+    per = -(-n // 64)
+    # every block has a size of its own, so that a maximum taken from another block gives another scale
+    size = 2.0 ** g.integers(-8, 9, per).repeat(64)[:n, None, None]
+    k, v = g.standard_normal((n, heads, 64)) * size, g.standard_normal((n, heads, 64)) / size
+    if plant is not None:
+        plant(k, v)
+    kd, vd = _dev(k, torch.bfloat16), _dev(v, torch.bfloat16)
+    codes = torch.full((batch * per, heads, 2, 4096), 0x33, dtype=torch.uint8, device="cuda")
+    scales = torch.full((batch * per, heads, 2), 0.25, device="cuda")
+    table = g.permutation(batch * per).reshape(batch, per)
+    given = table.copy()
+    given[:, [j for j in range(per) if bad(j)]] = -1
+    given[1::2, [j for j in range(per) if bad(j)]] = batch * per
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    B.cache_append(kd, vd, _i32([0] * batch), _i32([n] * batch), _i32([0] * batch), _i32(given), codes, scales, n, status=status)
+    w_codes, w_scales = np.full((per, heads, 2, 4096), 0x33, np.uint8), np.full((per, heads, 2), 0.25)
+    R.append(w_codes, w_scales, np.arange(per)[None], _host(kd), _host(vd), [0], [n], [0])
+    for j in range(per):
+        if bad(j):
+            w_codes[j], w_scales[j] = 0x33, 0.25
+    at = torch.from_numpy(table.reshape(-1)).cuda()
+    got_c, got_s = codes[at].view(batch, per, heads, 2, 4096), scales[at].view(batch, per, heads, 2)
+    assert torch.equal(got_s, _dev(w_scales.astype(np.float32)).expand_as(got_s))
+    assert torch.equal(got_c, _dev(w_codes).expand_as(got_c))
+    return status.item()
+
+
+@pytest.mark.parametrize("every", [2, 3])
+def test_append_bad_blocks_between_good_ones(every):
+    """600 (sequence, head) pairs of 79 blocks, 15 CTAs a pair: a CTA walks five or six blocks, some of them out of range."""
+    for seed in range(3):
+        assert _same_rows_everywhere(75, 8, 5000, lambda j: j % every == 1, seed) == -1
+    assert _same_rows_everywhere(75, 8, 5000, lambda j: j // 15 % every == 1, 3) == -1
+
+
+def test_append_many_blocks_per_cta():
+    """3200 (sequence, head) pairs: two CTAs walk the seven blocks of a pair, one of them with an infinity."""
+    def plant(k, v):
+        k[200, 3, 7], v[260, 5, 9] = math.inf, -math.inf
+        k[64 * 6, :, :] = 0.0
+    assert _same_rows_everywhere(200, 16, 64 * 6 + 40, lambda j: False, 5, plant) == 0
