@@ -476,6 +476,7 @@ PD_API pd_status pd_cache_append(int32_t dtype, int32_t batch, int32_t n_kv_head
  * key head h / (n_heads / n_kv_heads).
  *   dtype      PD_DTYPE_FP32 or PD_DTYPE_BF16: element type of q and out.  bf16: scores and sums in fp32, weights rounded to f16 (11 bits);
  *              fp32: queries and weights in two f16 parts (22 bits)
+ *   softcap    0: none.  Capped scores are off by a few last places of their own; bf16 with a cap of at most 64: by up to 2^-21 of the cap
  *   sizes      rows_per_seq 1..64; n_heads a multiple of n_kv_heads, at most 1024; max_len >= 0: host bound on lens, sizes the launch
  *   q          device, row (b, r) at (b * rows_per_seq + r) * q_stride (at least n_heads * 64, a multiple of 16 bytes), 16-byte aligned
  *   out        device [batch * rows_per_seq, n_heads * 64], 16-byte aligned

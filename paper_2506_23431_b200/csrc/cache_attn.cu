@@ -56,10 +56,15 @@ __host__ __device__ constexpr int smem_bytes(bool f32) { return ring_bytes(f32) 
 constexpr uint32_t kSpinLimit = 1u << 24;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLift = 15.f;                     // weights are 2^(s - max + kLift): at most 2^15 in f16
+// Largest cap whose tanh is taken as a quotient where weights are f16: the quotient is a difference of numbers near the cap, and a score is off by up to 2^-21 of the cap,
+// whatever its own size - 2^-15 at this one, an eighth of the weights' rounding.  tanhf is off by its own last place (32 x 16 heads x 2048 tokens, 12 rows: no cap 28.4 us,
+// quotient 34.3, tanhf 40.7).
+constexpr float kQuotientCap = 64.f;
 
 struct CacheAttnArgs {
   int R, H, HK, G, n_blocks, max_blocks, max_len, tiles, cluster, outer, n_bias;
-  float scale_log2e, cap_log2e, inv_cap;          // cap_log2e = 0: no cap; inv_cap = 2 * scale / cap * log2(e) (bf16) or scale / cap (fp32)
+  float scale_log2e, cap_log2e, inv_cap;          // cap_log2e = 0: no cap; inv_cap = scale / cap, by quotient 2 * scale / cap * log2(e)
+  bool cap_by_quotient;                           // tanh(x) = 1 - 2 / (1 + e^2x) instead of tanhf(x)
   const void *q; long long q_row;                 // row b * R + r of the queries at (b * R + r) * q_row
   const uint8_t *codes; const float2 *scales; const int32_t *table, *n_rows, *lens; const int2 *spans; const float *bias;
   void *out; float *part; int32_t *status;
@@ -363,13 +368,17 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(sizeof(T) == 4)) cache_a
       Row &w = row[x];
       const float mul = fmaxf(w.mul * sc.x, FLT_MIN);                              // a zero would make a masked score no number
       if (MOD && a.cap_log2e > 0.f) {
+        if (NP == 1 && a.cap_by_quotient) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
+          for (int j = 0; j < 8; ++j)
 #pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const float v = s[j][2 * x + e] * mul;
-            s[j][2 * x + e] = NP == 2 ? a.cap_log2e * tanhf(v) : fmaf(-2.f * a.cap_log2e, rcp(1.f + ex2(v)), a.cap_log2e);
-          }
+            for (int e = 0; e < 2; ++e) s[j][2 * x + e] = fmaf(-2.f * a.cap_log2e, rcp(1.f + ex2(s[j][2 * x + e] * mul)), a.cap_log2e);
+        } else {
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) s[j][2 * x + e] = a.cap_log2e * tanhf(s[j][2 * x + e] * mul);
+        }
       } else if (MOD) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) { s[j][2 * x] *= mul; s[j][2 * x + 1] *= mul; }
@@ -716,8 +725,8 @@ pd_status pd_cache_attention(int32_t dtype, int32_t batch, int32_t rows_per_seq,
   a.R = rows_per_seq; a.H = n_heads; a.HK = n_kv_heads; a.G = n_heads / n_kv_heads; a.n_blocks = n_blocks; a.max_blocks = max_blocks; a.max_len = max_len;
   a.tiles = p.tiles; a.cluster = p.cluster; a.outer = p.outer; a.n_bias = bias ? n_bias : 0;
   a.scale_log2e = attn_scale * kLog2e; a.cap_log2e = softcap * kLog2e;
-  // tanh(x) = 1 - 2 / (1 + e^2x): the bf16 kernel wants 2 x in log2 units
-  a.inv_cap = softcap > 0.f ? (dtype == PD_DTYPE_BF16 ? 2.f * kLog2e : 1.f) * attn_scale / softcap : 0.f;
+  a.cap_by_quotient = dtype == PD_DTYPE_BF16 && softcap <= kQuotientCap;
+  a.inv_cap = softcap > 0.f ? (a.cap_by_quotient ? 2.f * kLog2e : 1.f) * attn_scale / softcap : 0.f;
   a.q = q; a.q_row = q_stride; a.codes = static_cast<const uint8_t *>(codes); a.scales = reinterpret_cast<const float2 *>(scales);
   a.table = table; a.n_rows = n_rows; a.lens = lens; a.spans = reinterpret_cast<const int2 *>(spans); a.bias = bias;
   a.out = out; a.part = static_cast<float *>(scratch); a.status = status;

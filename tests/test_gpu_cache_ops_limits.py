@@ -6,7 +6,7 @@ import numpy as np
 import pytest
 
 from tests import cache_reference as R
-from tests.test_gpu_cache_ops import _dev, _host, _i32
+from tests.test_gpu_cache_ops import HALF, _attend, _dev, _dt, _filled, _host, _i32
 
 pytestmark = pytest.mark.gpu
 
@@ -59,3 +59,38 @@ def test_append_many_blocks_per_cta():
         k[200, 3, 7], v[260, 5, 9] = math.inf, -math.inf
         k[64 * 6, :, :] = 0.0
     assert _same_rows_everywhere(200, 16, 64 * 6 + 40, lambda j: False, 5, plant) == 0
+
+
+# ---- attention: caps of any size -------------------------------------------------------------------------------
+def _dense(c, n, kv):
+    """Keys and values of the one sequence of a cache, float64 [kv heads, n, 64]."""
+    at = c.table[0, :-(-n // 64)]
+    val = R.VALUES[c.codes[at]] * np.asarray(c.scales, np.float64)[at][..., None]
+    k = val[:, :, 0].reshape(-1, kv, 64, 64).transpose(1, 0, 2, 3).reshape(kv, -1, 64)[:, :n]
+    v = val[:, :, 1].reshape(-1, kv, 64, 64).transpose(1, 0, 3, 2).reshape(kv, -1, 64)[:, :n]
+    return k, v
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("cap", [65.0, 1e3, 1e5, 1e8, 1e20, 9e29])
+def test_large_caps(dtype, cap):
+    """A cap far above the scores is as good as none: a score's error goes by the score, not by the cap.
+
+    The bound is that of the plain form with 2^-21 |score| in the cap's place: a sum of 64 products (2^-17 + 2^-22 of the summed
+    magnitudes), scaling 2^-24 twice, tanh 2^-22 and its product 2^-24, all below 2^-20 |score|."""
+    lens, rows, heads, kv = [300], 4, 4, 2
+    c = _filled(61, lens, kv)
+    q = _dev(np.random.default_rng(62).standard_normal((1, rows, heads * 64)) * 2, _dt(dtype))
+    got = _host(_attend(c, q, [rows], lens, None, None, cap)).reshape(rows, heads, 64)
+    K, V = _dense(c, 300, kv)
+    for r in range(rows):
+        for h in range(heads):
+            qq, k, v = _host(q)[0, r, h * 64:h * 64 + 64], K[h * kv // heads], V[h * kv // heads]
+            s = 0.125 * (k @ qq)
+            err = 0.125 * ((2.0 ** -17 + 2.0 ** -22) * (np.abs(k) @ np.abs(qq)) + 2.0 ** -24 * np.abs(qq).max() * np.abs(k).sum(-1)) + 2.0 ** -20 * np.abs(s)
+            s = cap * np.tanh(s / cap)
+            w = np.exp(s - s.max())
+            w /= w.sum()
+            ref, mean = w @ v, w @ np.abs(v)
+            bound = HALF[dtype] * np.abs(ref) * 1.01 + mean * (2 * err.max() + 2.0 ** -16 + (2.0 ** -11 if dtype == "bf16" else 2.0 ** -22)) + 2.0 ** -40 * np.abs(v).sum(0)
+            assert (np.abs(got[r, h] - ref) <= bound).all(), f"{(np.abs(got[r, h] - ref) / bound).max():.1f} times the bound"
