@@ -490,6 +490,7 @@ PD_API pd_status pd_cache_append(int32_t dtype, int32_t batch, int32_t n_kv_head
  *              (256 bytes where no sequence is split: not touched then, and NULL with 0 bytes will do)
  *   status     device int32 or NULL: set to PD_ERR_ARG for a block outside 0 .. n_blocks among those that are read (its positions
  *              count as not there), to PD_ERR_TIMEOUT if a bounded wait inside the kernel expired; otherwise left alone
+ * Weighted values are summed in fp32 relative to a row's largest weight: a result is a number wherever the sum of the magnitudes that the row sees is one.
  * Codes behind a sequence's last token, and those that a row does not see, never matter, numbers or not.  Results repeat bit for bit; what the
  * other sequences of the batch hold does not change them (the sizes of the call set the order of the sums).  Enqueues on cuda_stream and returns; allocates nothing on the device.
  * PD_ERR_ARG for null pointers, misaligned buffers or sizes out of range, PD_ERR_WORKSPACE for a scratch that is

@@ -55,7 +55,11 @@ __host__ __device__ constexpr int ring_bytes(bool f32) { return kWarps * slots(f
 __host__ __device__ constexpr int smem_bytes(bool f32) { return ring_bytes(f32) + kInboxBytes + kWarps * (int)sizeof(WarpNotes); }
 constexpr uint32_t kSpinLimit = 1u << 24;
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kLift = 15.f;                     // weights are 2^(s - max + kLift): at most 2^15 in f16
+constexpr float kLift = 15.f, kDrop = 0x1p-15f;   // weights are 2^(s - max + kLift): at most 2^15 in f16; kDrop takes the lift out again
+// Sums of values keep the lift (the factor of a block of the smallest scales stays a normal number) until a warp meets a block of this scale: its lifted sums could overflow
+// where sums of the values do not.  Of smaller blocks 2^31 tokens cannot.  (Taking the lift out with every block's factor, and with its sums where the factor gets too
+// small: 32 x 16 heads x 2048 tokens 28.8 us instead of 28.0.)
+constexpr float kLarge = 0x1p64f;
 // Largest cap whose tanh is taken as a quotient where weights are f16: the quotient is a difference of numbers near the cap, and a score is off by up to 2^-21 of the cap,
 // whatever its own size - 2^-15 at this one, an eighth of the weights' rounding.  tanhf is off by its own last place (32 x 16 heads x 2048 tokens, 12 rows: no cap 28.4 us,
 // quotient 34.3, tanhf 40.7).
@@ -297,6 +301,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(sizeof(T) == 4)) cache_a
 
   // ---- the blocks
   bool ok = true;
+  float unit = 1.f;                                                                // of the sums of values: kDrop once there were large ones
   int st = 0; uint32_t phase = 0;                                                  // slot and phase of the copy that is waited for next
   auto arrived = [&] { return __all_sync(0xffffffffu, mbar_wait(bar0 + st * 8, phase)); };
   // The warp is through with copy c: its slot takes copy c + NS, which must not overtake the warp's reads.
@@ -439,12 +444,16 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(sizeof(T) == 4)) cache_a
     // ---- values, four tiles of eight dims at a time
     if (!(ok = arrived())) break;
     const uint32_t vbase = slot0 + st * kPart;
-    if (__any_sync(0xffffffffu, keep[0] != 1.f || keep[1] != 1.f)) {               // some row's running maximum moved
+    const bool large = sc.y >= kLarge && unit == 1.f;                              // lifted sums of such values could overflow where the values' own do not
+    if (large || __any_sync(0xffffffffu, keep[0] != 1.f || keep[1] != 1.f)) {      // some row's running maximum moved
+      const float f = large ? kDrop : 1.f;
 #pragma unroll
       for (int dn = 0; dn < 8; ++dn)
 #pragma unroll
-        for (int x = 0; x < 4; ++x) o[dn][x] *= keep[x >> 1];
+        for (int x = 0; x < 4; ++x) o[dn][x] *= keep[x >> 1] * f;
+      unit *= f;
     }
+    const float vscale = sc.y * unit;
     uint32_t nan_seen = 0;                                                         // values that are no numbers, at positions that some row sees
     if (here) {
 #pragma unroll
@@ -491,7 +500,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(sizeof(T) == 4)) cache_a
 #pragma unroll
         for (int dn = 0; dn < 4; ++dn)
 #pragma unroll
-          for (int x = 0; x < 4; ++x) o[dh + dn][x] = fmaf(tv[dn][x], take[x >> 1] * sc.y, o[dh + dn][x]);
+          for (int x = 0; x < 4; ++x) o[dh + dn][x] = fmaf(tv[dn][x], take[x >> 1] * vscale, o[dh + dn][x]);
       }
       if (edge && __any_sync(0xffffffffu, nan_seen != 0)) {
         // rows that see such a value get it after all: a product of who sees which position with where they stand
@@ -541,16 +550,17 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(sizeof(T) == 4)) cache_a
 
   // ---- join the warps, then the cluster's CTAs, both in their order: a thread takes columns 4 k .. 4 k + 3 and 32 + 4 k .. of a row
   __syncthreads();                                                                 // the rings are free
+  const float drop = unit == 1.f ? kDrop : 1.f;                                    // the lift leaves here at the latest
   float *rec = reinterpret_cast<float *>(ring), *ml = rec + kWarps * kRows * kDh;   // [warp][row][64], [warp][row][2]
 #pragma unroll
   for (int x = 0; x < 2; ++x) {
     const int m = warp * kRows + x * 8 + g;
     const int2 sp = notes.span[x * 8 + g];
     const bool any = sp.x < sp.y;                          // rows that see nothing went along unmasked
-    if (t == 0) store2(ml + 2 * m, any ? row[x].m : -INFINITY, any ? row[x].l : 0.f);
+    if (t == 0) store2(ml + 2 * m, any ? row[x].m : -INFINITY, any ? row[x].l * kDrop : 0.f);
 #pragma unroll
     for (int dn = 0; dn < 8; ++dn)
-      store2(rec + m * kDh + ((dn * 8 + 2 * t) ^ ((g & 3) << 3)), any ? o[dn][2 * x] : 0.f, any ? o[dn][2 * x + 1] : 0.f);
+      store2(rec + m * kDh + ((dn * 8 + 2 * t) ^ ((g & 3) << 3)), any ? o[dn][2 * x] * drop : 0.f, any ? o[dn][2 * x + 1] * drop : 0.f);
   }
   __syncthreads();
   const int cluster = a.cluster, rank = split % cluster, own = kRows / cluster;     // rank k sums rows k * own .. of the cluster's CTAs

@@ -6,7 +6,7 @@ import numpy as np
 import pytest
 
 from tests import cache_reference as R
-from tests.test_gpu_cache_ops import HALF, _attend, _dev, _dt, _filled, _host, _i32
+from tests.test_gpu_cache_ops import HALF, Cache, _attend, _dev, _dt, _filled, _host, _i32
 
 pytestmark = pytest.mark.gpu
 
@@ -94,3 +94,30 @@ def test_large_caps(dtype, cap):
             ref, mean = w @ v, w @ np.abs(v)
             bound = HALF[dtype] * np.abs(ref) * 1.01 + mean * (2 * err.max() + 2.0 ** -16 + (2.0 ** -11 if dtype == "bf16" else 2.0 ** -22)) + 2.0 ** -40 * np.abs(v).sum(0)
             assert (np.abs(got[r, h] - ref) <= bound).all(), f"{(np.abs(got[r, h] - ref) / bound).max():.1f} times the bound"
+
+
+# ---- attention: values, biases and scores of any size ----------------------------------------------------------
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("sizes", [[1e-35], [1e-30], [1e33], [1e35], [2e36], [1, 1e30, 1e-20, 1e36, 1], [1e19, 1e20, 1e25, 1e18, 1e22], [1e36, 1e-25, 1e-10, 1e-25, 1e-25]])
+def test_values_of_any_size(dtype, sizes):
+    """Sums of values are held relative to the row's largest weight: no size of values overflows whose sum over the tokens is a number, and small ones lose nothing.
+    One row sees all blocks, the others one block each, of a size of its own.
+
+    The bound is the plain form's, and what underflow adds: the factor of a block's values is off by half of 2^-149 where it is no normal number, its sums of
+    64 weights up to 2^15 times codes up to 448 turn that into 2^-120, and the lift of 2^15 goes again: 2^-135, sixteen blocks and the sum's roundings 2^-130; a result
+    below the normal range is off by half its spacing, 2^-134 in bf16.  Where a warp has met large values the lift has gone before: 2^-115 for the small blocks' rows."""
+    from paper_2506_23431_b200 import binding as B
+    n, rows = 1000, 6
+    g = np.random.default_rng(67)
+    c = Cache(67, 1, 16, 2)
+    v = g.standard_normal((n, 2, 64)) * np.resize(sizes, 16).repeat(64)[:n, None, None]
+    c.append(g.standard_normal((n, 2, 64)), v, [0], [n], [0], "fp32")
+    q = _dev(g.standard_normal((1, rows, 128)), _dt(dtype))
+    sp = np.array([[[0, n], [0, 64], [64, 128], [128, 192], [192, 256], [256, 300]]])
+    ref, mean, slack = R.attend(_host(q), c.codes, c.scales, c.table, [rows], [n], 0.125, sp)
+    bound = HALF[dtype] * np.abs(ref) * 1.01 + slack + mean * (2.0 ** -11 if dtype == "bf16" else 2.0 ** -22) + (2.0 ** -115 if max(sizes) > 1e18 else 2.0 ** -130)
+    for batch in (1, 300):                                         # a block for each warp, or four
+        got = _host(B.cache_attention(q.expand(batch, -1, -1).contiguous(), c.d_codes, c.d_scales, c.d_table.expand(batch, -1).contiguous(), _i32([rows] * batch), _i32([n] * batch), 0.125,
+                                      spans=_i32(np.repeat(sp, batch, 0))))
+        for b in (0, batch - 1):
+            assert np.isfinite(got[b]).all() and (np.abs(got[b] - ref[0]) <= bound[0]).all(), f"{np.nanmax(np.abs(got[b] - ref[0]) / bound[0]):.1f} times the bound"
