@@ -484,7 +484,8 @@ PD_API pd_status pd_cache_append(int32_t dtype, int32_t batch, int32_t n_kv_head
  *   spans      device int32 [batch, rows_per_seq, 2] = (begin, end) of every row, 8-byte aligned, clamped to 0..lens[b]; NULL = (0, lens[b]).
  *              A causal step: end = the row's own position + 1; windows, documents and prefixes likewise
  *   bias       device fp32 [n_heads, n_bias] or NULL: added by the distance from the end of the row's (clamped) span
- *              values below -2e38 count as minus infinity: such a position weighs nothing, and a row without others is zero
+ *              values below -2e38 count as minus infinity: such a position weighs nothing, and a row without others is zero; values
+ *              up to 2e38 are numbers, greater ones may overflow
  *   scratch    device, 16-byte aligned, at least pd_cache_attention_scratch_bytes(...): partial results where a sequence is split;
  *              needs no clearing, holds nothing between calls; calls that may overlap on the GPU need one each
  *              (256 bytes where no sequence is split: not touched then, and NULL with 0 bytes will do)

@@ -56,6 +56,8 @@ __host__ __device__ constexpr int smem_bytes(bool f32) { return ring_bytes(f32) 
 constexpr uint32_t kSpinLimit = 1u << 24;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLift = 15.f, kDrop = 0x1p-15f;   // weights are 2^(s - max + kLift): at most 2^15 in f16; kDrop takes the lift out again
+// A score whose bias is below -2e38 counts as minus infinity (scores without a bias are lost in its last place).
+constexpr float kGone = -2e38f * kLog2e;
 // Sums of values keep the lift (the factor of a block of the smallest scales stays a normal number) until a warp meets a block of this scale: its lifted sums could overflow
 // where sums of the values do not.  Of smaller blocks 2^31 tokens cannot.  (Taking the lift out with every block's factor, and with its sums where the factor gets too
 // small: 32 x 16 heads x 2048 tokens 28.8 us instead of 28.0.)
@@ -425,6 +427,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(sizeof(T) == 4)) cache_a
       for (int j = 0; j < 8; ++j) mx = fmaxf(mx, fmaxf(s[j][2 * x], s[j][2 * x + 1]));
       mx = quad_max(mx);
       if (!here) mx = -INFINITY;
+      if (MOD && a.bias && mx < kGone) mx = -INFINITY;                             // where others have more, such positions weigh nothing anyway
       const float f = MOD ? 1.f : mul;
       mx *= f;
       const float ref = kLift - (mx == -INFINITY ? 0.f : mx);

@@ -6,7 +6,7 @@ import numpy as np
 import pytest
 
 from tests import cache_reference as R
-from tests.test_gpu_cache_ops import HALF, Cache, _attend, _dev, _dt, _filled, _host, _i32
+from tests.test_gpu_cache_ops import HALF, Cache, _attend, _check, _dev, _dt, _filled, _host, _i32
 
 pytestmark = pytest.mark.gpu
 
@@ -121,3 +121,32 @@ def test_values_of_any_size(dtype, sizes):
                                       spans=_i32(np.repeat(sp, batch, 0))))
         for b in (0, batch - 1):
             assert np.isfinite(got[b]).all() and (np.abs(got[b] - ref[0]) <= bound[0]).all(), f"{np.nanmax(np.abs(got[b] - ref[0]) / bound[0]):.1f} times the bound"
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_bias_on_either_side_of_minus_infinity(dtype):
+    """Below -2e38 a bias removes the position; at and above it is a number like others: a row that has the same everywhere takes the values' mean (its scores are
+    far below the bias's last place)."""
+    lens, rows = [200], 2
+    c = _filled(71, lens, 2)
+    q = _dev(np.random.default_rng(72).standard_normal((1, rows, 128)), _dt(dtype))
+    _, V = _dense(c, 200, 2)
+    for low, gone in ((-2.2e38, True), (-2.01e38, True), (-2e38, False), (-1.9e38, False)):
+        bias = np.zeros((2, 3), np.float32)
+        bias[0] = low
+        got = _host(_attend(c, q, [rows], lens, None, bias, 0.0))
+        every = R.attend(_host(q), c.codes, c.scales, c.table, [rows], lens, 0.125)
+        _check(_dev(got[..., 64:]), tuple(w[..., 64:] for w in every), dtype)
+        if gone:
+            assert not got[..., :64].any()
+        else:
+            ref, mean = V[0].mean(0), np.abs(V[0]).mean(0)
+            assert (np.abs(got[..., :64] - ref) <= HALF[dtype] * np.abs(ref) * 1.01 + 2.0 ** -16 * mean).all()
+        bias[0] = [0.0, low, 0.0]                                  # one position removed: it weighs nothing either way
+        got = _host(_attend(c, q, [rows], lens, None, bias, 0.0))
+        K, _ = _dense(c, 200, 2)
+        s = 0.125 * np.einsum("rd,kd->rk", _host(q)[0, :, :64], K[0])
+        s[:, 198] = -math.inf
+        w = np.exp(s - s.max(-1, keepdims=True))
+        w /= w.sum(-1, keepdims=True)
+        assert np.abs(got[0, :, :64] - w @ V[0]).max() <= 2.0 ** -6 * np.abs(V[0]).max()
