@@ -150,3 +150,31 @@ def test_bias_on_either_side_of_minus_infinity(dtype):
         w = np.exp(s - s.max(-1, keepdims=True))
         w /= w.sum(-1, keepdims=True)
         assert np.abs(got[0, :, :64] - w @ V[0]).max() <= 2.0 ** -6 * np.abs(V[0]).max()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("size", [1e5, 4e6, 1.3e7, 3e7, 1e8, 7e9, 1e15, 1e25, 1e35])
+@pytest.mark.parametrize("mod", ["plain", "bias", "cap"])
+def test_scores_of_any_size(dtype, size, mod):
+    """Scores so large that neighbouring numbers lie further apart than a weight's range: the largest takes all, equal ones share.
+
+    Key p is a multiple of one direction: the chosen positions have the largest score, all others at most 0.9 of it (or, below zero, 1.1), which is a weight of nothing
+    at these sizes; equal keys have equal codes, so equal scores.  The result is the mean of the chosen values: the output's rounding and 2^-16 for its sums."""
+    from paper_2506_23431_b200 import binding as B
+    g = np.random.default_rng(int(math.log2(size)))
+    n, rows = 700, 3
+    for sign in (1, -1):
+        for chosen in ([5], [650], [3, 64, 200, 699]):
+            k = np.empty((n, 1, 64))
+            k[:] = (np.round(g.random((n, 1, 1)) * 8) / 16 if sign > 0 else 1.25 + np.round(g.random((n, 1, 1)) * 4) / 8)      # codes hold these exactly
+            k[chosen] = 1.0
+            c = Cache(73, 1, 11, 1)
+            c.append(k, g.standard_normal((n, 1, 64)), [0], [n], [0], "fp32")
+            q = _dev(np.full((1, rows, 64), sign * size / 64 * 8 * (1 + g.random())), _dt(dtype))
+            bias = np.zeros((1, 4), np.float32) if mod == "bias" else None
+            got = _host(B.cache_attention(q, c.d_codes, c.d_scales, c.d_table, _i32([rows]), _i32([n]), 0.125, bias=None if bias is None else _dev(bias),
+                                          softcap=9e29 if mod == "cap" and size < 1e28 else 0.0))
+            K, V = _dense(c, n, 1)
+            assert (K[0][chosen] == 1).all() and (np.delete(K[0], chosen, 0).max() <= 0.9 if sign > 0 else np.delete(K[0], chosen, 0).min() >= 1.1)
+            ref, mean = V[0][chosen].mean(0), np.abs(V[0][chosen]).mean(0)
+            assert (np.abs(got - ref) <= HALF[dtype] * np.abs(ref) * 1.01 + 2.0 ** -16 * mean).all(), (sign, chosen, got[0, 0, :4], ref[:4])
