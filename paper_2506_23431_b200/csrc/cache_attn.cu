@@ -73,8 +73,8 @@ constexpr float kQuotientCap = 64.f;
 
 struct CacheAttnArgs {
   int R, H, HK, G, n_blocks, max_blocks, max_len, tiles, cluster, outer, n_bias;
-  float scale_log2e, cap_log2e, inv_cap;          // cap_log2e = 0: no cap; inv_cap = scale / cap, by quotient 2 * scale / cap * log2(e)
-  bool cap_by_quotient;                           // tanh(x) = 1 - 2 / (1 + e^2x) instead of tanhf(x)
+  int cap;                                        // 0: none; tanh(x) as 1: 1 - 2 / (1 + e^2x), 2: tanhf(x)
+  float factor, cap_log2e;                        // of q . k: by cap scale * log2(e), 2 * scale / cap * log2(e), scale / cap
   const void *q; long long q_row;                 // row b * R + r of the queries at (b * R + r) * q_row
   const uint8_t *codes; const float2 *scales; const int32_t *table, *n_rows, *lens; const int2 *spans; const float *bias;
   void *out; float *part; int32_t *status;
@@ -186,7 +186,7 @@ __device__ __forceinline__ void store2(__nv_bfloat16 *p, float a, float b) { *re
 
 // One row of the tile that this lane holds columns of: its softmax so far.
 struct Row {
-  float mul;                        // score in log2 units (or the cap's argument) per unit of q . code at a key scale of 1
+  float unit;                       // of the queries as the tensor cores hold them: a power of two
   float m, l;
 };
 
@@ -288,7 +288,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(sizeof(T) == 4)) cache_a
     mx = quad_max(mx);
     const int e = min(max((int)(__float_as_uint(mx) >> 23) - 127, -126), 126);
     const float down = __uint_as_float((uint32_t)(127 - e) << 23);
-    w.mul = __uint_as_float((uint32_t)(127 + e) << 23) * (MOD && a.cap_log2e > 0.f ? a.inv_cap : a.scale_log2e);
+    w.unit = __uint_as_float((uint32_t)(127 + e) << 23);
 #pragma unroll
     for (int s = 0; s < 4; ++s)
 #pragma unroll
@@ -377,9 +377,11 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(sizeof(T) == 4)) cache_a
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
       Row &w = row[x];
-      const float mul = fmaxf(w.mul * sc.x, FLT_MIN);                              // a zero would make a masked score no number
-      if (MOD && a.cap_log2e > 0.f) {
-        if (NP == 1 && a.cap_by_quotient) {
+      // Score in log2 units (or the cap's argument) per unit of q . code.  The units of queries and keys first: one may be near the end of the range where the other is near its other
+      // end.  Neither a zero (times a masked score) nor an infinity (times a zero) may come of it
+      const float per = w.unit * sc.x * a.factor, mul = MOD ? fminf(per, FLT_MAX) : fmaxf(per, FLT_MIN);
+      if (MOD && a.cap) {
+        if (NP == 1 && a.cap == 1) {
 #pragma unroll
           for (int j = 0; j < 8; ++j)
 #pragma unroll
@@ -753,9 +755,9 @@ pd_status pd_cache_attention(int32_t dtype, int32_t batch, int32_t rows_per_seq,
   CacheAttnArgs a;
   a.R = rows_per_seq; a.H = n_heads; a.HK = n_kv_heads; a.G = n_heads / n_kv_heads; a.n_blocks = n_blocks; a.max_blocks = max_blocks; a.max_len = max_len;
   a.tiles = p.tiles; a.cluster = p.cluster; a.outer = p.outer; a.n_bias = bias ? n_bias : 0;
-  a.scale_log2e = attn_scale * kLog2e; a.cap_log2e = softcap * kLog2e;
-  a.cap_by_quotient = dtype == PD_DTYPE_BF16 && softcap <= kQuotientCap;
-  a.inv_cap = softcap > 0.f ? (a.cap_by_quotient ? 2.f * kLog2e : 1.f) * attn_scale / softcap : 0.f;
+  a.cap = softcap > 0.f ? (dtype == PD_DTYPE_BF16 && softcap <= kQuotientCap ? 1 : 2) : 0;
+  a.factor = std::min(attn_scale * (a.cap == 2 ? 1.f : a.cap ? 2.f * kLog2e : kLog2e) / (a.cap ? softcap : 1.f), FLT_MAX);
+  a.cap_log2e = softcap * kLog2e;
   a.q = q; a.q_row = q_stride; a.codes = static_cast<const uint8_t *>(codes); a.scales = reinterpret_cast<const float2 *>(scales);
   a.table = table; a.n_rows = n_rows; a.lens = lens; a.spans = reinterpret_cast<const int2 *>(spans); a.bias = bias;
   a.out = out; a.part = static_cast<float *>(scratch); a.status = status;

@@ -96,6 +96,18 @@ def test_large_caps(dtype, cap):
             assert (np.abs(got[r, h] - ref) <= bound).all(), f"{(np.abs(got[r, h] - ref) / bound).max():.1f} times the bound"
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_small_caps_and_scores(dtype):
+    """A cap at which every score saturates, and scores of nothing."""
+    lens = [200]
+    c = _filled(63, lens, 2)
+    q = _dev(np.random.default_rng(64).standard_normal((1, 3, 128)) * 2, _dt(dtype))
+    for cap in (1e-3, 1e-30, 1e-44):
+        _check(_attend(c, q, [3], lens, None, None, cap), R.attend(_host(q), c.codes, c.scales, c.table, [3], lens, 0.125, cap=cap), dtype)
+        zero = q * 0
+        _check(_attend(c, zero, [3], lens, None, None, cap), R.attend(_host(zero), c.codes, c.scales, c.table, [3], lens, 0.125, cap=cap), dtype)
+
+
 # ---- attention: values, biases and scores of any size ----------------------------------------------------------
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("sizes", [[1e-35], [1e-30], [1e33], [1e35], [2e36], [1, 1e30, 1e-20, 1e36, 1], [1e19, 1e20, 1e25, 1e18, 1e22], [1e36, 1e-25, 1e-10, 1e-25, 1e-25]])
@@ -178,3 +190,18 @@ def test_scores_of_any_size(dtype, size, mod):
             assert (K[0][chosen] == 1).all() and (np.delete(K[0], chosen, 0).max() <= 0.9 if sign > 0 else np.delete(K[0], chosen, 0).min() >= 1.1)
             ref, mean = V[0][chosen].mean(0), np.abs(V[0][chosen]).mean(0)
             assert (np.abs(got - ref) <= HALF[dtype] * np.abs(ref) * 1.01 + 2.0 ** -16 * mean).all(), (sign, chosen, got[0, 0, :4], ref[:4])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_large_queries_with_a_large_scale(dtype):
+    """Queries near the end of the range over keys near the other, and a scale above one: the scores are ordinary numbers."""
+    from paper_2506_23431_b200 import binding as B
+    g = np.random.default_rng(79)
+    lens, rows = [200], 3
+    for size, scale in ((1e38, 4.0), (1e37, 30.0), (1e30, 1e4), (1e-30, 1e4)):
+        c = Cache(79, 1, 5, 2)
+        c.append(g.standard_normal((200, 2, 64)) / size / scale * 0.2, g.standard_normal((200, 2, 64)), [0], lens, [0], "fp32")
+        q = _dev(np.clip(g.standard_normal((1, rows, 128)), -3, 3) * size, _dt(dtype))
+        for cap, bias in ((0.0, None), (0.0, np.zeros((2, 3), np.float32)), (20.0, None)):
+            got = B.cache_attention(q, c.d_codes, c.d_scales, c.d_table, _i32([rows]), _i32(lens), scale, softcap=cap, bias=None if bias is None else _dev(bias))
+            _check(got, R.attend(_host(q), c.codes, c.scales, c.table, [rows], lens, scale, bias=bias, cap=cap), dtype)
