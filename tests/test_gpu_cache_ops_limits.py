@@ -205,3 +205,19 @@ def test_large_queries_with_a_large_scale(dtype):
         for cap, bias in ((0.0, None), (0.0, np.zeros((2, 3), np.float32)), (20.0, None)):
             got = B.cache_attention(q, c.d_codes, c.d_scales, c.d_table, _i32([rows]), _i32(lens), scale, softcap=cap, bias=None if bias is None else _dev(bias))
             _check(got, R.attend(_host(q), c.codes, c.scales, c.table, [rows], lens, scale, bias=bias, cap=cap), dtype)
+
+
+# ---- counts of zero, sizes at the end of 32 bits, launches that fail -------------------------------------------
+def test_append_counts_that_its_sizes_do_not_allow():
+    """No rows, or no new tokens allowed: a sequence that has some all the same is reported, as with any other bound."""
+    import torch
+    from paper_2506_23431_b200 import binding as B
+    c = _filled(83, [70], 2)
+    before = c.d_codes.clone()
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    for rows, n, most, want in ((5, 0, 0, 0), (0, 0, 0, 0), (0, 0, 7, 0), (5, 3, 0, -1), (0, 3, 7, -1), (0, 3, 0, -1)):
+        status.zero_()
+        k = torch.ones(rows, 2, 64, dtype=torch.bfloat16, device="cuda")
+        B.cache_append(k, k, _i32([0]), _i32([n]), _i32([70]), c.d_table, c.d_codes, c.d_scales, most, status=status)
+        assert status.item() == want, (rows, n, most)
+    assert torch.equal(c.d_codes, before)
