@@ -237,7 +237,7 @@ __global__ void __launch_bounds__(kRotThreads, 4) rotary_staged_kernel(RotaryArg
 
 template <typename T>
 cudaError_t launch_rotary_staged(const RotaryArgs &a, int interleaved, cudaStream_t s) {
-  const int grid = (a.tokens + a.tok_per_cta - 1) / a.tok_per_cta;
+  const int grid = (a.tokens - 1) / a.tok_per_cta + 1;
   return op_launch(interleaved ? rotary_staged_kernel<T, true> : rotary_staged_kernel<T, false>, dim3(grid), kRotThreads, 0, 1, s, a);
 }
 
@@ -248,7 +248,7 @@ cudaError_t launch_rotary(const RotaryArgs &a, int interleaved, cudaStream_t s) 
   // whole groups of a token's items, or even shares of them, so that few threads have none
   const long long shares = (per_tok + kRotThreads - 1) / kRotThreads, busy = shares > 1 ? (per_tok + shares - 1) / shares : kRotThreads / per_tok * per_tok;
   const int threads = (int)((busy + 31) / 32 * 32);
-  const int grid = (a.tokens + a.tok_per_cta - 1) / a.tok_per_cta;
+  const int grid = (a.tokens - 1) / a.tok_per_cta + 1;
   return op_launch(interleaved ? rotary_kernel<T, true, VEC> : rotary_kernel<T, false, VEC>, dim3(grid), threads, 0, 1, s, a);
 }
 

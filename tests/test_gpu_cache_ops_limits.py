@@ -221,3 +221,20 @@ def test_append_counts_that_its_sizes_do_not_allow():
         B.cache_append(k, k, _i32([0]), _i32([n]), _i32([70]), c.d_table, c.d_codes, c.d_scales, most, status=status)
         assert status.item() == want, (rows, n, most)
     assert torch.equal(c.d_codes, before)
+
+
+def test_rotary_of_the_most_tokens():
+    """2^31 - 1 tokens of one head of two dims: the same as a call on a few of them."""
+    import torch
+    from paper_2506_23431_b200 import binding as B
+    n = (1 << 31) - 1
+    if torch.cuda.mem_get_info()[0] < 20 << 30:
+        pytest.skip("needs 18 GB")
+    x = torch.randn(1, 1, 2, device="cuda").bfloat16().expand(n, 1, 2)
+    pos = torch.arange(n, dtype=torch.int32, device="cuda")
+    turns = _dev(np.array([0.0123456789]))
+    out = torch.empty(n, 1, 2, dtype=torch.bfloat16, device="cuda")
+    B.rotary(x, pos, turns, out=out)
+    for at in (0, 1 << 20, (1 << 30) - 500, n - 1000):
+        few = slice(at, at + 1000)
+        assert torch.equal(out[few], B.rotary(x[few], pos[few], turns))
