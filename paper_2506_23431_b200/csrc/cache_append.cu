@@ -277,5 +277,5 @@ extern "C" pd_status pd_cache_append(int32_t dtype, int32_t batch, int32_t n_kv_
   const dim3 grid(n_kv_heads, (unsigned)std::min(65535ll, std::max(1ll, std::min(blocks, kAppendCtas / pairs))), batch);
   cudaStream_t s = reinterpret_cast<cudaStream_t>(cuda_stream);
   const cudaError_t st = op_launch(dtype == PD_DTYPE_BF16 ? cache_append_kernel<__nv_bfloat16> : cache_append_kernel<float>, grid, 128, 0, 1, s, a);
-  return st == cudaSuccess ? PD_OK : PD_ERR_CUDA;
+  return op_status(st);
 }

@@ -766,7 +766,7 @@ pd_status pd_cache_attention(int32_t dtype, int32_t batch, int32_t rows_per_seq,
   cudaError_t st;
   if (dtype == PD_DTYPE_FP32) st = launch_cache_attn<float>(a, batch, mod, s);
   else st = launch_cache_attn<__nv_bfloat16>(a, batch, mod, s);
-  return st == cudaSuccess ? PD_OK : PD_ERR_CUDA;
+  return op_status(st);
 }
 
 }  // extern "C"

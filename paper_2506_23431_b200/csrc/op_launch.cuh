@@ -4,6 +4,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include "pd.h"
+
 namespace pd {
 
 // Whether every address (null ones among them) is a multiple of n.
@@ -33,6 +35,13 @@ cudaError_t op_launch(void (*kernel)(P...), dim3 grid, int threads, size_t smem,
   cfg.attrs = attr;
   cfg.numAttrs = cluster > 1 ? 2 : 1;
   return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
+// What an entry point returns.  A refused launch is the caller's to handle by that alone: CUDA's own note of it would come up in the next check anyone makes.
+inline pd_status op_status(cudaError_t st) {
+  if (st == cudaSuccess) return PD_OK;
+  cudaGetLastError();
+  return PD_ERR_CUDA;
 }
 
 }  // namespace pd

@@ -324,7 +324,7 @@ pd_status pd_rotary(int32_t dtype, int32_t tokens, int32_t n_heads, int32_t d_he
   else
     st = whole(16) ? launch_rotary<float, 4>(a, interleaved, s) : by_eight ? launch_rotary<float, 2>(a, interleaved, s)
        : pieces(16) ? launch_rotary_staged<float>(a, interleaved, s) : launch_rotary<float, 1>(a, interleaved, s);
-  return st == cudaSuccess ? PD_OK : PD_ERR_CUDA;
+  return op_status(st);
 }
 
 }  // extern "C"

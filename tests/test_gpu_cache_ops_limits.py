@@ -1,5 +1,6 @@
 """The operators around the 8-bit paged cache at the ends of what their documentation allows: caps, biases, scores and values of any
 size, bad blocks between good ones, walks of many blocks, counts of zero, launches that fail."""
+import ctypes as C
 import math
 
 import numpy as np
@@ -238,3 +239,34 @@ def test_rotary_of_the_most_tokens():
     for at in (0, 1 << 20, (1 << 30) - 500, n - 1000):
         few = slice(at, at + 1000)
         assert torch.equal(out[few], B.rotary(x[few], pos[few], turns))
+
+
+def test_a_failed_launch_leaves_no_error_behind():
+    """A launch on the default stream while a stream that waits for it is captured is refused by CUDA; the caller's next check of its own must not see that."""
+    import torch
+    from paper_2506_23431_b200 import binding as B
+    x = torch.randn(4, 3, 64, device="cuda").bfloat16()
+    pos, turns, out = _i32([1, 2, 3, 4]), _dev(B.rotary_turns(64)[0]), torch.zeros(4, 3, 64, device="cuda").bfloat16()
+    c = _filled(89, [70], 2)
+    q, n, le, one, zero = torch.randn(1, 2, 128, device="cuda").bfloat16(), _i32([2]), _i32([70]), _i32([1]), _i32([0])
+    kv = torch.randn(1, 2, 64, device="cuda").bfloat16()
+    res = torch.empty_like(q)
+    want = B.cache_attention(q, c.d_codes, c.d_scales, c.d_table, n, le, 0.125)
+    torch.cuda.synchronize()
+    rt = C.CDLL("libcudart.so.12")
+    p = lambda t: C.c_void_p(t.data_ptr())  # noqa: E731
+    calls = [lambda: B._lib.pd_rotary(1, 4, 3, 64, 64, 0, 0, p(x), 192, 64, p(pos), p(turns), 1.0, p(out), 192, 64, None),
+             lambda: B._lib.pd_cache_append(1, 1, 2, c.codes.shape[0], c.d_table.shape[1], 1, 1, p(kv), 128, p(kv), 128, p(zero), p(one), p(le), p(c.d_table), p(c.d_codes), p(c.d_scales),
+                                            None, None),
+             lambda: B._lib.pd_cache_attention(1, 1, 2, 2, 2, c.codes.shape[0], c.d_table.shape[1], 70, 0.125, 0.0, p(q), 128, p(c.d_codes), p(c.d_scales), p(c.d_table), p(n), p(le), None,
+                                               None, 0, p(res), None, 0, None, None)]
+    for call in calls:
+        s, graph = C.c_void_p(), C.c_void_p()
+        assert rt.cudaStreamCreate(C.byref(s)) == 0
+        assert rt.cudaStreamBeginCapture(s, 2) == 0                          # 2: relaxed
+        status, left = call(), rt.cudaPeekAtLastError()
+        rt.cudaStreamEndCapture(s, C.byref(graph))
+        rt.cudaGetLastError()
+        assert rt.cudaStreamDestroy(s) == 0
+        assert status == -5 and left == 0
+    assert torch.equal(B.cache_attention(q, c.d_codes, c.d_scales, c.d_table, n, le, 0.125), want)
