@@ -263,18 +263,20 @@ pd_status pd_rotary_turns(int32_t rot_dim, double theta, int32_t scaling, double
   if (scaling != PD_ROTARY_PLAIN && (!(factor >= 1.0) || !isfinite(factor))) return PD_ERR_ARG;
   const double two_pi = 6.283185307179586476925;
   double lo = 0.0, hi = 0.0;
+  bool all_slow = false;                               // even the first pair, which makes one turn in 2 pi positions: the ramp would leave it as it is
   if (scaling == PD_ROTARY_BY_PARTS) {
     if (original_len < 1 || !(slow_turns > 0.0) || !(fast_turns >= slow_turns) || !isfinite(fast_turns)) return PD_ERR_ARG;
     // pair index (of rot_dim / 2, as a real number) that makes `n` turns over the original context: theta^(-2 i / rot) L / (2 pi) = n
     auto pair_of = [&](double n) { return rot_dim * log(original_len / (n * two_pi)) / (2.0 * log(theta)); };
     lo = fmax(floor(pair_of(fast_turns)), 0.0);
     hi = fmin(ceil(pair_of(slow_turns)), rot_dim - 1.0);
+    all_slow = original_len / two_pi <= slow_turns && original_len / two_pi < fast_turns;
   }
   for (int i = 0; i < rot_dim / 2; ++i) {
     double f = pow(theta, -2.0 * i / rot_dim);
     if (scaling == PD_ROTARY_LINEAR) f /= factor;
     if (scaling == PD_ROTARY_BY_PARTS) {
-      const double ramp = fmin(fmax((i - lo) / fmax(hi - lo, 1e-3), 0.0), 1.0);
+      const double ramp = all_slow ? 1.0 : fmin(fmax((i - lo) / fmax(hi - lo, 1e-3), 0.0), 1.0);
       f = f / factor * ramp + f * (1.0 - ramp);
     }
     turns[i] = f / two_pi;

@@ -1,0 +1,19 @@
+"""Host side of the operators around the 8-bit paged cache at the ends of what their documentation allows (no GPU is touched)."""
+import math
+
+import numpy as np
+import pytest
+
+from paper_2506_23431_b200 import binding as B
+
+
+@pytest.mark.parametrize("original,fast,slow", [(4, 32.0, 1.0), (6, 32.0, 1.0), (100, 64.0, 16.5), (1, 1e-3, 1e-4), (7, 32.0, 1.0), (4096, 32.0, 1.0), (4096, 1.0, 1.0), (4, 1.0, 1.0), (1 << 20, 1e9, 1e8)])
+def test_frequencies_by_parts_at_the_first_pair(original, fast, slow):
+    """Every pair that makes at most `slow` turns over the original context is divided, the first one too; every one that makes at least `fast` is not."""
+    factor = 8.0
+    turns, _ = B.rotary_turns(64, 10000.0, B.PD_ROTARY_BY_PARTS, factor, original, fast, slow)
+    base = 10000.0 ** (-np.arange(32) / 32) / (2 * math.pi)
+    made = base * original
+    few, many = (made <= slow) & (made < fast), made >= fast
+    assert np.allclose(turns[few], base[few] / factor, rtol=1e-14) and np.allclose(turns[many], base[many], rtol=1e-14)
+    assert ((turns <= base * (1 + 1e-14)) & (turns >= base / factor * (1 - 1e-14))).all()
