@@ -552,6 +552,14 @@ def _op_start(t):
     return dt, dev, _Torch.stream(dev)
 
 
+_INT32_MAX = (1 << 31) - 1
+
+
+def _wide(*sizes):
+    """ValueError for sizes that the C call would take modulo 2^32 (ctypes does not look)."""
+    raise ValueError(f"sizes must fit 32 bits, got {sizes}")
+
+
 def _plain(what: str, t, dev: int, dtype, shape):
     """The address of a contiguous tensor of this type and shape on device `dev`, or ValueError."""
     if t.dtype is not dtype or t.shape != shape or t.get_device() != dev or not t.is_contiguous():
@@ -562,6 +570,8 @@ def _plain(what: str, t, dev: int, dtype, shape):
 def rotary_turns(rot_dim: int, theta: float = 10000.0, scaling: int = PD_ROTARY_PLAIN, factor: float = 1.0, original_len: int = 0,
                  fast_turns: float = 32.0, slow_turns: float = 1.0):
     """pd_rotary_turns: (turns per position of every pair, float64 numpy [rot_dim / 2]; amplitude)."""
+    if max(rot_dim, original_len, -rot_dim, -original_len) > _INT32_MAX:
+        _wide(rot_dim, original_len)
     turns = np.empty((max(int(rot_dim), 0) // 2,), np.float64)
     amp = C.c_float(0)
     st = _lib.pd_rotary_turns(rot_dim, theta, scaling, factor, original_len, fast_turns, slow_turns,
@@ -588,6 +598,8 @@ def rotary(x, positions, turns, amplitude: float = 1.0, interleaved: bool = Fals
     if (one != 1 or o_one != 1) and dh > 1:
         raise ValueError("the dims of a head must be neighbours")
     half = turns.shape[0]
+    if n > _INT32_MAX or half > _INT32_MAX // 2:
+        _wide(n, half)
     st = _lib.pd_rotary(dt, n, heads, dh, 2 * half, interleaved, inverse, x.data_ptr(), xt, xh, _plain("positions", positions, dev, _Torch.int32, (n,)),
                         _plain("turns", turns, dev, _Torch.float64, (half,)), amplitude, out.data_ptr(), ot, oh, stream)
     if st != PD_OK:
@@ -601,6 +613,8 @@ def _cache_args(codes, scales, table, dev: int):
         raise ValueError("codes must be [blocks, kv heads, 2, 4096], table [batch, blocks of a sequence]")
     n_blocks, heads = codes.shape[:2]
     batch, max_blocks = table.shape
+    if batch > _INT32_MAX or max_blocks > _INT32_MAX:
+        _wide(batch, max_blocks)
     return (n_blocks, heads, batch, max_blocks, _plain("codes", codes, dev, _Torch.uint8, (n_blocks, heads, 2, PD_CACHE_BLOCK * 64)),
             _plain("scales", scales, dev, _Torch.float32, (n_blocks, heads, 2)), _plain("table", table, dev, _Torch.int32, (batch, max_blocks)))
 
@@ -610,6 +624,8 @@ def cache_append(k, v, row_start, n_new, pos_start, table, codes, scales, max_ne
     int32 [batch], table int32 [batch, blocks], codes uint8 [blocks, kv heads, 2, 4096] and scales float32 [blocks, kv heads, 2],
     both written in place; max_new: host bound on n_new; status: int32 [1] or None.  Runs on torch's current stream of the
     current device, where all tensors are."""
+    if not -_INT32_MAX <= max_new <= _INT32_MAX:
+        _wide(max_new)
     dt, dev, stream = _op_start(k)
     n_blocks, heads, batch, max_blocks, cp, sp, tp = _cache_args(codes, scales, table, dev)
     rows = k.shape[0]
@@ -633,6 +649,9 @@ def cache_append(k, v, row_start, n_new, pos_start, table, codes, scales, max_ne
 @functools.lru_cache(maxsize=256)
 def cache_attention_scratch_bytes(dtype: int, batch: int, rows_per_seq: int, n_heads: int, n_kv_heads: int, max_len: int) -> int:
     """pd_cache_attention_scratch_bytes: a function of sizes alone (0: a size out of range)."""
+    sizes = dtype, batch, rows_per_seq, n_heads, n_kv_heads, max_len
+    if max(sizes) > _INT32_MAX or min(sizes) < -_INT32_MAX:
+        _wide(*sizes)
     return int(_lib.pd_cache_attention_scratch_bytes(dtype, batch, rows_per_seq, n_heads, n_kv_heads, max_len))
 
 
@@ -643,6 +662,8 @@ def cache_attention(q, codes, scales, table, n_rows, lens, attn_scale: float, ma
     None; max_len: host bound on lens (the table's extent when not given).  `out` [batch, rows, heads * 64] and `scratch`
     (16-byte aligned) are allocated here when not given.  Runs on torch's current stream of the current device, where all
     tensors are; returns out."""
+    if max_len is not None and not -_INT32_MAX <= max_len <= _INT32_MAX:
+        _wide(max_len)
     dt, dev, stream = _op_start(q)
     n_blocks, kv_heads, t_batch, max_blocks, cp, sp, tp = _cache_args(codes, scales, table, dev)
     if q.dim() != 3:
@@ -675,6 +696,8 @@ def cache_attention(q, codes, scales, table, n_rows, lens, attn_scale: float, ma
         if bias.dim() != 2:
             raise ValueError("bias must be [heads, distances]")
         n_bias = bias.shape[1]
+        if n_bias > _INT32_MAX:
+            _wide(n_bias)
         bias_ptr = _plain("bias", bias, dev, _Torch.float32, (heads, n_bias))
     st = _lib.pd_cache_attention(dt, batch, rows, heads, kv_heads, n_blocks, max_blocks, max_len, attn_scale, softcap, q.data_ptr(), stride, cp, sp, tp,
                                  _plain("n_rows", n_rows, dev, i32, per), _plain("lens", lens, dev, i32, per),

@@ -17,3 +17,19 @@ def test_frequencies_by_parts_at_the_first_pair(original, fast, slow):
     few, many = (made <= slow) & (made < fast), made >= fast
     assert np.allclose(turns[few], base[few] / factor, rtol=1e-14) and np.allclose(turns[many], base[many], rtol=1e-14)
     assert ((turns <= base * (1 + 1e-14)) & (turns >= base / factor * (1 - 1e-14))).all()
+
+
+def test_binding_refuses_sizes_beyond_32_bits():
+    """A size that the C call would take modulo 2^32 (and silently do something else) is refused before anything else is looked at."""
+    import torch
+    q, k, i32 = torch.zeros(1, 2, 128), torch.zeros(4, 2, 64), torch.zeros(1, dtype=torch.int32)
+    codes, scales, table = torch.zeros(3, 2, 2, 4096, dtype=torch.uint8), torch.ones(3, 2, 2), torch.zeros(1, 3, dtype=torch.int32)
+    for wide in ((1 << 32) + 100, 1 << 32, 1 << 31, -(1 << 32) + 100):
+        with pytest.raises(ValueError, match="32 bits"):
+            B.cache_attention(q, codes, scales, table, i32, i32, 0.125, max_len=wide)
+        with pytest.raises(ValueError, match="32 bits"):
+            B.cache_append(k, k, i32, i32, i32, table, codes, scales, wide)
+        with pytest.raises(ValueError, match="32 bits"):
+            B.cache_attention_scratch_bytes(1, 1, 2, 2, 2, wide)
+        with pytest.raises(ValueError, match="32 bits"):
+            B.rotary_turns(64, 10000.0, B.PD_ROTARY_BY_PARTS, 4.0, wide)

@@ -241,6 +241,18 @@ def test_rotary_of_the_most_tokens():
         assert torch.equal(out[few], B.rotary(x[few], pos[few], turns))
 
 
+def test_rotary_refuses_more_tokens_than_32_bits_hold():
+    """Not the remainder modulo 2^32: nothing is written."""
+    import torch
+    from paper_2506_23431_b200 import binding as B
+    n = (1 << 32) + 3
+    x = torch.ones(1, 1, 2, device="cuda").bfloat16().expand(n, 1, 2)
+    out = torch.zeros(1, 1, 2, device="cuda").bfloat16()
+    with pytest.raises(ValueError, match="32 bits"):
+        B.rotary(x, torch.zeros(1, dtype=torch.int32, device="cuda").expand(n), _dev(np.array([0.1])), out=out.expand(n, 1, 2))
+    assert not out.any()
+
+
 def test_a_failed_launch_leaves_no_error_behind():
     """A launch on the default stream while a stream that waits for it is captured is refused by CUDA; the caller's next check of its own must not see that."""
     import torch
