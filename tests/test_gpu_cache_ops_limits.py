@@ -62,6 +62,30 @@ def test_append_many_blocks_per_cta():
     assert _same_rows_everywhere(200, 16, 64 * 6 + 40, lambda j: False, 5, plant) == 0
 
 
+# ---- attention: walks of many blocks --------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype,batch,kv,blocks", [("bf16", 131, 2, 20), ("bf16", 131, 2, 36), ("bf16", 65, 4, 70), ("fp32", 97, 2, 36), ("fp32", 49, 4, 70)])
+def test_attention_of_many_blocks_per_warp(dtype, batch, kv, blocks):
+    """So many segments that each is one CTA's: its four warps take the blocks in turn, some tens each, in runs of 16 with tails of every kind.  The sequences
+    share the blocks of one (what an entry of the table names is read afresh by every warp) and differ in length."""
+    import torch
+    from paper_2506_23431_b200 import binding as B
+    most = 4 * blocks * 64
+    g = np.random.default_rng(blocks)
+    c = _filled(53, [64 * 40], kv)                                 # forty blocks, named again and again in another order
+    named = np.concatenate([g.permutation(c.table[0, :40]) for _ in range(-(-4 * blocks // 40))])[:4 * blocks]
+    table = np.repeat(named[None], batch, axis=0)
+    lens = most - (np.arange(batch) * 97) % (most // 2)
+    lens[:5] = most, most - 63, most - 64, most - 64 * 4, 64 * 4 * (blocks - 1) + 1
+    q = _dev(g.standard_normal((batch, 1, kv * 64)) * 0.7, _dt(dtype))
+    out = B.cache_attention(q, c.d_codes, c.d_scales, _i32(table), _i32(np.ones(batch)), _i32(lens), 0.125)
+    some = [0, 1, 2, 3, 4, batch // 2, batch - 1]
+    _check(out[some], R.attend(_host(q[some]), c.codes, c.scales, table[some], [1] * len(some), lens[some], 0.125), dtype)
+    # a window far into the walk
+    spans = np.stack([lens - 1000, lens - 3], -1)[:, None]
+    out = B.cache_attention(q, c.d_codes, c.d_scales, _i32(table), _i32(np.ones(batch)), _i32(lens), 0.125, spans=_i32(spans))
+    _check(out[some], R.attend(_host(q[some]), c.codes, c.scales, table[some], [1] * len(some), lens[some], 0.125, spans[some]), dtype)
+
+
 # ---- attention: caps of any size -------------------------------------------------------------------------------
 def _dense(c, n, kv):
     """Keys and values of the one sequence of a cache, float64 [kv heads, n, 64]."""
