@@ -148,7 +148,7 @@ __global__ void __launch_bounds__(128, sizeof(T) == 2 ? 7 : 4) cache_append_kern
   const int32_t *table = a.table + (size_t)b * a.max_blocks;
   const int j1 = (int)((end - 1) / kBlk);
   int turn = 0;
-  for (int j = p0 / kBlk + blockIdx.y; j <= j1; j += gridDim.y) {                 // blocks of the sequence
+  for (int j = p0 / kBlk + blockIdx.y; j <= j1; j += gridDim.y, turn ^= 1) {      // blocks of the sequence
     const int lo = max(p0 - j * kBlk, 0), hi = (int)min(end - (long long)j * kBlk, (long long)kBlk);
     const int id = j < a.max_blocks ? table[j] : -1;
     auto is_new = [&](int w, int k) { return tg[w] * 4 + k >= lo && tg[w] * 4 + k < hi; };
@@ -164,6 +164,7 @@ __global__ void __launch_bounds__(128, sizeof(T) == 2 ? 7 : 4) cache_append_kern
     }
     if (id < 0 || id >= a.n_blocks) {                                             // the same in all threads
       if (threadIdx.x == 0 && a.status) *a.status = PD_ERR_ARG;
+      __syncthreads();                                                            // a half of warp_max is written again behind the barrier of the block between only
       continue;
     }
     const size_t block = (size_t)id * a.heads + h;
@@ -249,7 +250,6 @@ __global__ void __launch_bounds__(128, sizeof(T) == 2 ? 7 : 4) cache_append_kern
       }
     }
     if (t == 0) reinterpret_cast<float2 *>(a.scales)[block] = make_float2(scale[0], scale[1]);
-    turn ^= 1;                                                                    // here only: a half is written again behind the barrier of the block after, and a skipped one has none
   }
 }
 
