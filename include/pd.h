@@ -417,7 +417,7 @@ PD_API const char *pd_static_last_error(void);
  * with t -> -t if inverse (the map's transpose: the gradient of x from that of y).  Angles are reduced in 64 bits: far positions
  * are as exact as near ones.
  *   dtype       PD_DTYPE_FP32 or PD_DTYPE_BF16: element type of x and out; the arithmetic is fp32, rounded once
- *   sizes       tokens >= 0; d_head 2..256; rot_dim even, 2..d_head
+ *   sizes       tokens >= 0; n_heads 1..65535; d_head 2..256; rot_dim even, 2..d_head
  *   x, out      device; element (token, head, dim) at token * token_stride + head * head_stride + dim (strides in elements, not
  *               negative; x may repeat, heads of out must not overlap).  Slices of a fused projection's rows will do.  out may be x
  *               with the same strides, else they must not overlap.  Fastest with addresses, strides and d_head that
@@ -443,16 +443,17 @@ PD_API pd_status pd_rotary(int32_t dtype, int32_t tokens, int32_t n_heads, int32
  * (block, head, keys | values).  kv_c_dtype = PD_KV_E4M3 has one scale for a sequence's whole context, which must be
  * there before the first code is written; here tokens can follow one by one, and a block of large values spoils no other.
  *   codes   device uint8 [n_blocks, n_kv_heads, 2, 4096], 16-byte aligned: a block's keys as [token][64], then its values as [64][token]
- *   scales  device fp32 [n_blocks, n_kv_heads, 2], powers of two: value = code * scale
+ *   scales  device fp32 [n_blocks, n_kv_heads, 2], 8-byte aligned, powers of two: value = code * scale
  *   table   device int32 [batch, max_blocks]: position p of sequence b is token p % PD_CACHE_BLOCK of block table[b][p / PD_CACHE_BLOCK]
  *
  * pd_cache_append writes positions pos_start[b] .. pos_start[b] + n_new[b] - 1 of every sequence from rows row_start[b] .. of k and v:
  *   scale = the least 2^e, e >= -126, with max |new value of the block| <= 448 * 2^e; where the block holds older tokens
  *           of the sequence, not less than its scale so far, and their codes are rounded to the new one
  *   code  = the nearest E4M3 value to value / scale, ties to even (NaN stays NaN; infinities set no scale and become 448)
- * Tokens of the block behind the new ones, other blocks and their scales stay as they were.  Both scales and codes are exact: they depend
+ * Codes of the block behind the new tokens, other blocks and their scales stay as they were.  (A block has one scale: what stood behind the new tokens is read
+ * at the new one.  Positions are appended in ascending order, or again from an earlier one on.)  Both scales and codes are exact: they depend
  * on the values and on how the tokens were split over calls (through the older codes), on nothing else.
- *   dtype      PD_DTYPE_FP32 or PD_DTYPE_BF16: element type of k and v
+ *   dtype      PD_DTYPE_FP32 or PD_DTYPE_BF16: element type of k and v;  batch, n_kv_heads 1..65535
  *   k, v       device [rows, n_kv_heads, 64], 16-byte aligned; k_stride, v_stride elements from row to row (at least
  *              n_kv_heads * 64, multiples of 16 bytes): slices of a fused projection will do
  *   row_start, n_new, pos_start   device int32 [batch]; n_new <= max_new (host), which sizes the launch; n_new = 0: nothing
@@ -460,7 +461,7 @@ PD_API pd_status pd_rotary(int32_t dtype, int32_t tokens, int32_t n_heads, int32
  *              n_new is above max_new or pos_start negative (the sequence is skipped), or a block lies behind the table or
  *              outside 0 .. n_blocks (its tokens are dropped).  Nothing outside the tensors is touched
  * With rows or max_new 0 nothing is written: k, v, table, codes and scales may be NULL, and without a status nothing is launched.
- * A block belongs to one sequence of a call, and calls that write one block are ordered by the caller.
+ * A block belongs to one sequence of a call and stands once among those that it writes; calls that write one block are ordered by the caller.
  * Enqueues on cuda_stream and returns; allocates nothing on the device.  PD_ERR_ARG for null pointers, misaligned
  * buffers or sizes out of range, PD_ERR_CUDA if a launch fails. */
 enum { PD_CACHE_BLOCK = 64 };
@@ -476,15 +477,16 @@ PD_API pd_status pd_cache_append(int32_t dtype, int32_t batch, int32_t n_kv_head
  * and is zero where it sees nothing; rows at or beyond n_rows[b] may hold anything and come back as zeros.  Query head h reads
  * key head h / (n_heads / n_kv_heads).
  *   dtype      PD_DTYPE_FP32 or PD_DTYPE_BF16: element type of q and out.  bf16: scores and sums in fp32, weights rounded to f16 (11 bits);
- *              fp32: queries and weights in two f16 parts (22 bits)
- *   softcap    0: none.  Capped scores are off by a few last places of their own; bf16 with a cap of at most 64: by up to 2^-21 of the cap
- *   sizes      rows_per_seq 1..64; n_heads a multiple of n_kv_heads, at most 1024; max_len >= 0: host bound on lens, sizes the launch
+ *              fp32: queries and weights in two f16 parts (22 bits).  A query's values are off by at most 2^-25 of its largest besides
+ *   attn_scale greater than 0, below 1e30
+ *   softcap    0: none; below 1e30.  Capped scores are off by a few last places of their own; bf16 with a cap of at most 64: by up to 2^-21 of the cap
+ *   sizes      batch 1..65535; rows_per_seq 1..64; n_heads a multiple of n_kv_heads, at most 1024; max_len >= 0: host bound on lens, sizes the launch
  *   q          device, row (b, r) at (b * rows_per_seq + r) * q_stride (at least n_heads * 64, a multiple of 16 bytes), 16-byte aligned
  *   out        device [batch * rows_per_seq, n_heads * 64], 16-byte aligned
  *   n_rows, lens   device int32 [batch]; clamped to 0..rows_per_seq and to 0..min(max_len, max_blocks * PD_CACHE_BLOCK)
  *   spans      device int32 [batch, rows_per_seq, 2] = (begin, end) of every row, 8-byte aligned, clamped to 0..lens[b]; NULL = (0, lens[b]).
  *              A causal step: end = the row's own position + 1; windows, documents and prefixes likewise
- *   bias       device fp32 [n_heads, n_bias] or NULL: added by the distance from the end of the row's (clamped) span
+ *   bias       device fp32 [n_heads, n_bias] or NULL, n_bias 1..2^20: added by the distance from the end of the row's (clamped) span
  *              values below -2e38 count as minus infinity: such a position weighs nothing, and a row without others is zero; values
  *              up to 2e38 are numbers, greater ones may overflow
  *   scratch    device, 16-byte aligned, at least pd_cache_attention_scratch_bytes(...): partial results where a sequence is split;

@@ -17,9 +17,9 @@
 // block of tiny weights and large values loses nothing.  32-bit queries and weights go through two f16 parts (22 bits), each with its own sums.
 //
 // Sixteen warps per SM with four independent products each: with eight warps and products in chains a launch of 32 sequences x 16 heads x 2048 tokens, 12
-// rows, took 56 us, now 28.4 (134 MB, 4.8 TB/s; every further 2048 tokens 21.3 us, 6.3 TB/s: what is left is the launch, one round of loads, and the last
-// blocks' work and join).  Loads alone take 25.  1 x 12 heads x 777 tokens 5.6 us, 2 x 4 key heads x 131072 tokens 31.2, of which 2.3 the merge of eight clusters.
-// A cap costs 2 us in 13, a bias over the table's distances as much.
+// rows, took 56 us, now 28.3 (134 MB, 4.8 TB/s; every further 2048 tokens 21.3 us, 6.3 TB/s: what is left is the launch, one round of loads, and the last
+// blocks' work and join).  Loads alone take 25.  1 x 12 heads x 777 tokens 5.7 us, 2 x 4 key heads x 131072 tokens 31.1, of which 2.3 the merge of eight clusters.
+// A cap costs 2 us in 14, a bias over the table's distances 2.5 in 13.  At 128 registers the bf16 forms spill 24 bytes per thread (fp32 8, with cap or bias 4).
 #include <cuda_fp16.h>
 #include <float.h>
 #include <limits.h>
@@ -43,7 +43,7 @@ constexpr int kMaxCluster = 8, kClusterSms = 128;
 constexpr int kOuterBlocks = 2;
 constexpr int kRows = 16;                         // rows of a tile
 // CTAs per SM as the registers allow (128 a thread; two f16 parts 168), and slots of 4 KB (a block's keys, or its values) in a warp's ring: what then
-// fits the shared memory (a fifth of a kilobyte more per CTA and one fewer is resident: 28 -> 37 us).
+// fits the shared memory (one CTA fewer per SM: 28 -> 37 us).
 __host__ __device__ constexpr int ctas_per_sm(bool f32) { return f32 ? 3 : 4; }
 __host__ __device__ constexpr int slots(bool f32) { return f32 ? 4 : 3; }
 constexpr int kRec = kDh + 4;                     // a row's partial result: 64 sums, maximum, sum of weights, alignment
@@ -53,6 +53,8 @@ constexpr int kRun = 16;
 struct WarpNotes { float2 scale[2 * kRun]; int id[2 * kRun]; int2 span[kRows]; uint64_t bar[4]; };
 __host__ __device__ constexpr int ring_bytes(bool f32) { return kWarps * slots(f32) * kPart; }
 __host__ __device__ constexpr int smem_bytes(bool f32) { return ring_bytes(f32) + kInboxBytes + kWarps * (int)sizeof(WarpNotes); }
+constexpr bool all_resident(bool f32) { return (smem_bytes(f32) + 1024) * ctas_per_sm(f32) <= 228 * 1024; }      // of 228 KB per SM each CTA takes 1 KB besides
+static_assert(all_resident(false) && all_resident(true), "shared memory for ctas_per_sm CTAs");
 constexpr uint32_t kSpinLimit = 1u << 24;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLift = 15.f, kDrop = 0x1p-15f;   // weights are 2^(s - max + kLift): at most 2^15 in f16; kDrop takes the lift out again
@@ -558,7 +560,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(sizeof(T) == 4)) cache_a
     float sum[4];
     mma_f16_first(sum, pf[0][0], 0x3c003c00u, 0x3c003c00u);
 #pragma unroll
-    for (int i = 1; i < 4 * NP; ++i) mma_f16(sum, pf[i >> 2][i & 3], 0x3c003c00u, 0x3c003c00u);
+    for (int k = 1; k < 4 * NP; ++k) mma_f16(sum, pf[k >> 2][k & 3], 0x3c003c00u, 0x3c003c00u);
 #pragma unroll
     for (int x = 0; x < 2; ++x)
       if (here) row[x].l = row[x].l * keep[x] + sum[2 * x] * take[x];
@@ -748,7 +750,6 @@ pd_status pd_cache_attention(int32_t dtype, int32_t batch, int32_t rows_per_seq,
   if (q_stride < (int64_t)n_heads * kDh || (q_stride * e) % 16 != 0) return PD_ERR_ARG;
   if (!aligned_to(16, q, codes, out, scratch) || !aligned_to(8, scales, spans) || !aligned_to(4, table, n_rows, lens, bias, status)) return PD_ERR_ARG;
   const Plan p = plan_of(dtype, batch, rows_per_seq, n_heads, n_kv_heads, max_len);
-  if ((long long)n_kv_heads * p.tiles > 65535) return PD_ERR_ARG;
   const size_t need = scratch_bytes_of(p, batch, n_kv_heads);
   if (need && !scratch) return PD_ERR_ARG;
   if (scratch_bytes < need) return PD_ERR_WORKSPACE;

@@ -13,7 +13,8 @@ template <typename... P>
 bool aligned_to(uintptr_t n, P... p) { return ((reinterpret_cast<uintptr_t>(p) | ...) % n) == 0; }
 
 // Everything enqueued before is complete and visible behind this; the kernel's first instruction.  What follows it in the stream may then be brought
-// onto the SMs while the kernel runs, up to its own wait: 1 to 2 us per launch between two of these operators.
+// onto the SMs while the kernel runs, up to its own wait: 1.3 to 2.2 us per launch between two of these operators in a stream (a step's three 13.4 us, without 18.5); in a
+// graph, whose launches are as close by themselves, nothing (12.9 and 12.8).
 __device__ __forceinline__ void op_begin() {
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");

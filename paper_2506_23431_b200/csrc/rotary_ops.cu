@@ -6,8 +6,9 @@
 // A frequency is held as turns per position in 64 bits: the product with the position keeps its fraction of a turn to 2^-52 of
 // the product, so that position 10^6 is as exact as position 1, and sincospif gets an argument in [-1, 1].  Sine and cosine
 // belong to a (token, pair), not to a head: a CTA computes those of its tokens once into shared memory and then streams all
-// heads through it, 16 bytes per load.  One read and one write of every element: HBM-bound for prompts (65536 x 32 bf16 heads 83.8 us,
-// 6.4 TB/s, 98 % of the copy rate; with loads of one token at a time 99.5), one launch latency for a decode step (2.2 us).
+// heads through it, 16 bytes per load.  One read and one write of every element: HBM-bound for prompts (65536 x 32 bf16 heads 83.8 us in a graph,
+// 6.4 TB/s, 98 % of the copy rate; calls on changing buffers up to 94 us, 5.7 TB/s, 87 %; with loads of one token at a time 99.5), one launch latency for a decode
+// step (2.2 us).  The bf16 form by halves spills 24 bytes per thread at its 64 registers.
 #include <math.h>
 
 #include "op_launch.cuh"
