@@ -460,7 +460,8 @@ PD_API pd_status pd_rotary(int32_t dtype, int32_t tokens, int32_t n_heads, int32
  *   status     device int32 or NULL: set to PD_ERR_ARG, and otherwise left alone, when a sequence's rows are not within 0 .. rows,
  *              n_new is above max_new or pos_start negative (the sequence is skipped), or a block lies behind the table or
  *              outside 0 .. n_blocks (its tokens are dropped).  Nothing outside the tensors is touched
- * With rows or max_new 0 nothing is written: k, v, table, codes and scales may be NULL, and without a status nothing is launched.
+ * With rows or max_new 0 nothing is written and only the counts are checked, for a status: k, v, table, codes and scales may be anything, and without a status
+ * nothing is launched.
  * A block belongs to one sequence of a call and stands once among those that it writes; calls that write one block are ordered by the caller.
  * Enqueues on cuda_stream and returns; allocates nothing on the device.  PD_ERR_ARG for null pointers, misaligned
  * buffers or sizes out of range, PD_ERR_CUDA if a launch fails. */

@@ -261,12 +261,15 @@ extern "C" pd_status pd_cache_append(int32_t dtype, int32_t batch, int32_t n_kv_
                                      void *codes, float *scales, int32_t *status, void *cuda_stream) {
   if (dtype != PD_DTYPE_FP32 && dtype != PD_DTYPE_BF16) return PD_ERR_ARG;
   if (batch < 1 || batch > 65535 || n_kv_heads < 1 || n_kv_heads > 65535 || n_blocks < 1 || max_blocks < 1 || rows < 0 || max_new < 0) return PD_ERR_ARG;
-  const bool nothing = max_new == 0 || rows == 0;                                  // a sequence with new tokens all the same is reported
-  if (nothing && !status) return PD_OK;
-  if (!row_start || !n_new || !pos_start || (!nothing && (!k || !v || !table || !codes || !scales))) return PD_ERR_ARG;
   const int e = dtype == PD_DTYPE_BF16 ? 2 : 4;
-  if (k_stride < (int64_t)n_kv_heads * kDh || v_stride < (int64_t)n_kv_heads * kDh || (k_stride * e) % 16 != 0 || (v_stride * e) % 16 != 0) return PD_ERR_ARG;
-  if (!aligned_to(16, k, v, codes) || !aligned_to(8, scales) || !aligned_to(4, row_start, n_new, pos_start, table, status)) return PD_ERR_ARG;
+  if (max_new == 0 || rows == 0) {                                                 // nothing to write; a sequence with new tokens all the same is reported
+    if (!status || !row_start || !n_new || !pos_start) return PD_OK;
+  } else {
+    if (!k || !v || !row_start || !n_new || !pos_start || !table || !codes || !scales) return PD_ERR_ARG;
+    if (k_stride < (int64_t)n_kv_heads * kDh || v_stride < (int64_t)n_kv_heads * kDh || (k_stride * e) % 16 != 0 || (v_stride * e) % 16 != 0) return PD_ERR_ARG;
+    if (!aligned_to(16, k, v, codes) || !aligned_to(8, scales) || !aligned_to(4, table)) return PD_ERR_ARG;
+  }
+  if (!aligned_to(4, row_start, n_new, pos_start, status)) return PD_ERR_ARG;
   AppendArgs a;
   a.heads = n_kv_heads; a.n_blocks = n_blocks; a.max_blocks = max_blocks; a.rows = rows; a.max_new = max_new;
   a.k = k; a.v = v; a.k_stride = k_stride; a.v_stride = v_stride;

@@ -33,3 +33,12 @@ def test_binding_refuses_sizes_beyond_32_bits():
             B.cache_attention_scratch_bytes(1, 1, 2, 2, 2, wide)
         with pytest.raises(ValueError, match="32 bits"):
             B.rotary_turns(64, 10000.0, B.PD_ROTARY_BY_PARTS, 4.0, wide)
+
+
+def test_append_of_nothing_looks_at_nothing_else():
+    """No rows, or no tokens allowed: strides, alignment and missing tensors are no error, with and without a status word (whose call checks counts only)."""
+    P = 1 << 20            # an address that is never followed: every call here returns before its launch
+    for rows, most in ((0, 5), (5, 0)):
+        for status in (None, P):
+            assert B._lib.pd_cache_append(1, 2, 3, 8, 4, rows, most, P + 2, 0, None, 1, None, P, P, None, P + 1, None, status, None) == 0
+        assert B._lib.pd_cache_append(1, 2, 3, 8, 4, rows, most, P + 2, 0, None, 1, P, P, P, None, P + 1, None, P + 2, None) == -1
