@@ -69,14 +69,15 @@ constexpr float kGone = -2e38f * kLog2e;
 // small: 32 x 16 heads x 2048 tokens 28.8 us instead of 28.0.)
 constexpr float kLarge = 0x1p64f;
 // Largest cap whose tanh is taken as a quotient where weights are f16: the quotient is a difference of numbers near the cap, and a score is off by up to 2^-21 of the cap,
-// whatever its own size - 2^-15 at this one, an eighth of the weights' rounding.  tanhf is off by its own last place (32 x 16 heads x 2048 tokens, 12 rows: no cap 28.4 us,
-// quotient 34.3, tanhf 40.7).
+// whatever its own size - 2^-15 at this one, an eighth of the weights' rounding.  tanhf is off by its own last place (32 x 16 heads x 2048 tokens, 12 rows: no cap 28.3 us,
+// quotient 35.2, tanhf 41.7).
 constexpr float kQuotientCap = 64.f;
 
 struct CacheAttnArgs {
   int R, H, HK, G, n_blocks, max_blocks, max_len, tiles, cluster, outer, n_bias;
   int cap;                                        // 0: none; tanh(x) as 1: 1 - 2 / (1 + e^2x), 2: tanhf(x)
-  float factor, cap_log2e;                        // of q . k: by cap scale * log2(e), 2 * scale / cap * log2(e), scale / cap
+  float factor, cap_log2e, inv_cap;               // of q . k: scale * log2(e), by quotient 2 * scale / cap * log2(e); 1 / cap_log2e, a step of its own in tanhf's argument, since
+                                                  // scale / cap may be too small for a number where the scores are not
   const void *q; long long q_row;                 // row b * R + r of the queries at (b * R + r) * q_row
   const uint8_t *codes; const float2 *scales; const int32_t *table, *n_rows, *lens; const int2 *spans; const float *bias;
   void *out; float *part; int32_t *status;
@@ -392,7 +393,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(sizeof(T) == 4)) cache_a
 #pragma unroll
           for (int j = 0; j < 8; ++j)
 #pragma unroll
-            for (int e = 0; e < 2; ++e) s[j][2 * x + e] = a.cap_log2e * tanhf(s[j][2 * x + e] * mul);
+            for (int e = 0; e < 2; ++e) s[j][2 * x + e] = a.cap_log2e * tanhf(s[j][2 * x + e] * mul * a.inv_cap);
         }
       } else if (MOD) {
 #pragma unroll
@@ -757,8 +758,9 @@ pd_status pd_cache_attention(int32_t dtype, int32_t batch, int32_t rows_per_seq,
   a.R = rows_per_seq; a.H = n_heads; a.HK = n_kv_heads; a.G = n_heads / n_kv_heads; a.n_blocks = n_blocks; a.max_blocks = max_blocks; a.max_len = max_len;
   a.tiles = p.tiles; a.cluster = p.cluster; a.outer = p.outer; a.n_bias = bias ? n_bias : 0;
   a.cap = softcap > 0.f ? (dtype == PD_DTYPE_BF16 && softcap <= kQuotientCap ? 1 : 2) : 0;
-  a.factor = std::min(attn_scale * (a.cap == 2 ? 1.f : a.cap ? 2.f * kLog2e : kLog2e) / (a.cap ? softcap : 1.f), FLT_MAX);
+  a.factor = a.cap == 1 ? std::min(2.f * kLog2e * attn_scale / softcap, FLT_MAX) : attn_scale * kLog2e;
   a.cap_log2e = softcap * kLog2e;
+  a.inv_cap = a.cap ? std::min(1.f / a.cap_log2e, FLT_MAX) : 0.f;
   a.q = q; a.q_row = q_stride; a.codes = static_cast<const uint8_t *>(codes); a.scales = reinterpret_cast<const float2 *>(scales);
   a.table = table; a.n_rows = n_rows; a.lens = lens; a.spans = reinterpret_cast<const int2 *>(spans); a.bias = bias;
   a.out = out; a.part = static_cast<float *>(scratch); a.status = status;

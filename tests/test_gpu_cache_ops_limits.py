@@ -232,6 +232,30 @@ def test_large_queries_with_a_large_scale(dtype):
             _check(got, R.attend(_host(q), c.codes, c.scales, c.table, [rows], lens, scale, bias=bias, cap=cap), dtype)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("size,scale,cap", [(1e20, 1e-30, 9e29), (1e30, 1e-25, 1e25), (1e-30, 1e25, 1e-30), (1e-20, 1e29, 1e29), (1.0, 1e-38, 100.0), (1.0, 1e-38, 50.0)])
+def test_scales_far_from_their_caps(dtype, size, scale, cap):
+    """The quotient of scale and cap may be no number of 32 bits: the scores are.  Large caps are as good as none (the plain form without one, whose own term of the bound, 2^-21 of
+    a score, is doubled by tanh); a tiny one leaves scores of nothing, and every position weighs the same."""
+    from paper_2506_23431_b200 import binding as B
+    g = np.random.default_rng(97)
+    lens, rows = [200], 3
+    c = Cache(97, 1, 5, 2)
+    c.append(np.clip(g.standard_normal((200, 2, 64)) / size / scale * 0.2, -3e38, 3e38), g.standard_normal((200, 2, 64)), [0], lens, [0], "fp32")
+    q = _dev(np.clip(g.standard_normal((1, rows, 128)), -3, 3) * size, _dt(dtype))
+    got = B.cache_attention(q, c.d_codes, c.d_scales, c.d_table, _i32([rows]), _i32(lens), scale, softcap=cap)
+    if cap < 1e-20:
+        ref = np.concatenate([v.mean(0) for v in _dense(c, 200, 2)[1]])
+        assert (np.abs(_host(got)[0] - ref) <= HALF[dtype] * np.abs(ref) * 1.01 + 2.0 ** -16 * np.abs(_dense(c, 200, 2)[1]).mean((0, 1)).max()).all()
+    elif cap <= 1e3:
+        _check(got, R.attend(_host(q), c.codes, c.scales, c.table, [rows], lens, scale, cap=cap), dtype)
+    else:
+        s = scale * np.einsum("rhd,hkd->rhk", _host(q)[0].reshape(rows, 2, 64), _dense(c, 200, 2)[0])
+        assert np.abs(s).max() ** 3 / cap ** 2 < 2.0 ** -20
+        out, mean, slack = R.attend(_host(q), c.codes, c.scales, c.table, [rows], lens, scale)
+        _check(got, (out, mean, 2 * slack), dtype)
+
+
 # ---- counts of zero, sizes at the end of 32 bits, launches that fail -------------------------------------------
 def test_append_counts_that_its_sizes_do_not_allow():
     """No rows, or no new tokens allowed: a sequence that has some all the same is reported, as with any other bound."""
